@@ -275,6 +275,79 @@ int fc_op_window_attention_noalloc(const void *q, const void *kcache, const void
                                    int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_seq,
                                    int32_t max_len, int32_t dtype, void *cuda_stream);
 
+/* ---- paged K/V cache: what writes it, reads it and manages its pages ----
+ * The paper keeps one cache per question; these operations keep one pool of pages for many.  A few-shot prompt ("Experiment
+ * Settings") is cached once and shared by the questions behind it, sequences take slots as they grow, and a sliding window with a few
+ * first tokens that stay visible bounds what a long rationale reads.  (Paper: "Overview of FastCoT", "Cache Update"; pages are this
+ * library's addition.)
+ *
+ * A pool holds n_pages pages of page_size slots for every layer and kv head.  Element i of the key in (layer, page, kv head, slot) is
+ * k[layer * layer_stride + page * page_stride + head * head_stride + slot * slot_stride + i], the value likewise from v: pages may be
+ * laid out [kv head][slot] or [slot][kv head], padded, or with K and V taking turns.  The slab of a context is such a pool too, with
+ * max_seq slots per page and a page per sequence.
+ * Sequences are rows of a table, device int32 [n_seqs, table_width]: entry i is the page of positions i * page_size ..; -1: none.
+ * kv_len, device int32 [n_seqs]: committed tokens; -1: the row holds no sequence.  refs, device int32 [n_pages]: table entries that
+ * hold the page; 0: free.  The caller owns all of it and starts with tables of -1, kv_len -1, refs 0.
+ *
+ * Unlike the other operations these calls only enqueue work on cuda_stream (no wait, no allocation, no copy from host memory that
+ * the caller has to keep), so they can be captured; lengths, tables and reference counts are read on the device when the work runs.  The
+ * current device must be the one that the pointers and the stream belong to.  Calls that change a table, kv_len, refs or pages must be
+ * ordered with their readers, and calls that share scratch with one another, by the stream or by events. */
+typedef struct {
+  void *k, *v;                /* DEVICE, 16-byte aligned */
+  int32_t dtype;              /* fc_dtype */
+  int32_t n_layers, n_pages, n_kv_heads, page_size, head_dim;   /* head_dim in {32, 64, 128}; any page_size >= 1 */
+  int64_t layer_stride, page_stride, head_stride, slot_stride;  /* elements; whole multiples of 16 bytes; rows must not overlap */
+} fc_pages;
+
+/* QKV rows -> queries and cached keys and values of one layer.  qkv: fp32 [batch * c] rows of (q | k | v), (n_heads + 2 n_kv_heads) *
+ * head_dim wide, qkv_stride elements apart.  Row b * c + j is position kv_len[b] + j: q and k are rotated (pairs i <-> i + head_dim/2,
+ * angle position * rope_theta^(-2i/head_dim), in 64 bits), k and v stored in the pool's type in their slot, q in q_out
+ * [batch * c, n_heads * head_dim] in the pool's type.  A row whose page is not in the pool stores no k and v; a row of the table
+ * without a sequence leaves everything as it was.  A page may be written by one row of the table only (fc_op_pages_reserve).
+ * c <= 64; pointers 16-byte aligned, qkv_stride a multiple of 4. */
+int fc_op_paged_store(const fc_pages *pages, int32_t layer, const int32_t *table, int32_t table_width, const int32_t *kv_len,
+                      const float *qkv, int64_t qkv_stride, void *q_out, int32_t batch, int32_t c, int32_t n_heads, float rope_theta,
+                      void *cuda_stream);
+
+/* Window attention of one layer over pages, as fc_op_window_attention: row b * c + j, at position p = kv_len[b] + j, sees the keys at
+ * positions t <= p; with window > 0 only those with t > p - window or t < n_sink.  c = 1 is the attention of one new token.  The window's own keys
+ * and values are in their slots already.  q: [batch * c] rows of n_heads * head_dim in the pool's type, q_stride elements apart; out: fp32
+ * [batch * c, n_heads * head_dim].  Rows of a table row without a sequence are 0.  A row that sees a key whose page is not in the
+ * pool, or lies beyond the table, is NaN; pages that no row sees may be missing.  Keys and values that a row does not see do not reach
+ * it, whatever they hold.  Results do not depend on the order in which the work runs.
+ * c <= 64; q, out 16-byte aligned, q_stride a multiple of 16 bytes; scratch: device, 256-byte aligned, at least
+ * ..._scratch_bytes(...) bytes (0: shape refused), whatever the lengths; what it holds before and after means nothing. */
+size_t fc_op_paged_attention_scratch_bytes(int32_t batch, int32_t c, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype);
+int fc_op_paged_attention(const fc_pages *pages, int32_t layer, const int32_t *table, int32_t table_width, const int32_t *kv_len,
+                          const void *q, int64_t q_stride, float *out, int32_t batch, int32_t c, int32_t n_heads, int32_t window,
+                          int32_t n_sink, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/* Share: table row dst[i] gives up the pages it holds and takes over kv_len and the pages of row src[i]'s committed tokens (one
+ * reference more each; nothing is copied).  src, dst: HOST [n], rows of the table; the dst are distinct and none is a src. */
+int fc_op_pages_fork(int32_t *table, int32_t table_width, int32_t n_seqs, int32_t *kv_len, int32_t *refs, int32_t n_pages,
+                     int32_t page_size, const int32_t *src, const int32_t *dst, int32_t n, void *cuda_stream);
+
+/* Make positions kv_len[b] .. kv_len[b] + rows - 1 of every sequence writable (rows <= 64).  Where there is no page it gets the lowest
+ * free one; a page that others hold too is replaced by a free one, its content copied in all layers if it has committed tokens.  Where all holders of a page are
+ * about to write it, the last of them (by table row) keeps it.  Sequences are served in the order of the table as long as pages last, each wholly or not at
+ * all; served: device int32 [n_seqs], nullable, 1 where the positions can be written; 0 also for rows without a sequence and for
+ * positions beyond the table.  scratch: device, 256-byte aligned, >= ..._scratch_bytes(...). */
+size_t fc_op_pages_reserve_scratch_bytes(int32_t n_pages, int32_t n_seqs);
+int fc_op_pages_reserve(const fc_pages *pages, int32_t *table, int32_t table_width, int32_t n_seqs, const int32_t *kv_len, int32_t *refs,
+                        int32_t rows, int32_t *served, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/* Release pages of the table rows seqs (HOST [n], distinct).  window == 0: all of them, and the row holds no sequence any more
+ * (kv_len -1).  window > 0: only pages that no row at position kv_len or later sees under that sliding window with n_sink sinks. */
+int fc_op_pages_free(int32_t *table, int32_t table_width, int32_t n_seqs, int32_t *kv_len, int32_t *refs, int32_t n_pages,
+                     int32_t page_size, const int32_t *seqs, int32_t n, int32_t window, int32_t n_sink, void *cuda_stream);
+
+/* Move the pages in use to the front of the pool: with n of them in use, the i-th one from page n on goes to the i-th free page below
+ * n, in all layers; table and refs follow, pages n .. n_pages - 1 are free afterwards.  n_live: device int32 [1], nullable, receives n. */
+size_t fc_op_pages_compact_scratch_bytes(int32_t n_pages);
+int fc_op_pages_compact(const fc_pages *pages, int32_t *table, int32_t table_width, int32_t n_seqs, int32_t *refs, int32_t *n_live,
+                        void *scratch, size_t scratch_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

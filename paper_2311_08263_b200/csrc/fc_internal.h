@@ -369,4 +369,7 @@ cudaError_t launch_gemm_chain(const UmmaPlan *const *plans, const GemmArgs *args
                               unsigned int *claim, unsigned int *bar_b, const ChainSync *sync, unsigned int *tile_done,
                               int td_stride, const ZeroList *zero, int pdl, cudaStream_t st, int cta_pairs = 0);
 
+// Paged K/V cache (k_pages.cu): FC_OK, or why a pool cannot be used.
+int pages_ok(const fc_pages *p);
+
 }  // namespace fc

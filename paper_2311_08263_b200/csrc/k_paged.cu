@@ -1,0 +1,206 @@
+// Paged K/V cache: rotation and K/V write into pages, window attention over pages.
+#include <climits>
+#include <cmath>
+#include <cstring>
+
+#include "fc_internal.h"
+#include "fc_paged.h"
+
+namespace fc {
+
+namespace {
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t *>(&v);
+}
+__device__ __forceinline__ void put4(float *p, const float (&v)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void put4(__nv_bfloat16 *p, const float (&v)[4]) {
+  *reinterpret_cast<uint2 *>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+}
+
+// ------------------------------------------------------------------------------------------------ store
+struct PagedStoreArgs {
+  PageView pool;
+  const int32_t *table; int width;
+  const int32_t *kv_len;
+  const float *qkv; long long qkv_stride;
+  void *q;
+  int c, hq, hd;
+  double turns[64];        // theta^(-2i/hd) / (2 pi): rotations of pair i from one position to the next
+};
+
+// A thread takes four adjacent pairs (i, i + hd/2) of one head of one row: 16-byte loads, 8- or 16-byte stores.  The angle in whole turns
+// is a 64-bit product whose integer part is dropped, so that far positions keep their fraction; what is left goes to sincospif.
+template <typename T>
+__global__ void __launch_bounds__(256) paged_store_kernel(const __grid_constant__ PagedStoreArgs a) {
+  const int r = blockIdx.x, b = r / a.c;
+  const int cap = a.width * a.pool.page_size;
+  if (a.kv_len[b] < 0) return;
+  const long long pos = (long long)a.kv_len[b] + (r - b * a.c);          // beyond the table: there is no page, q is rotated all the same
+  const int page = pos < cap ? page_of(a.table + (long long)b * a.width, a.width, (int)pos, a.pool.page_size, a.pool.n_pages) : -1;
+  const long long slot = (long long)page * a.pool.page_stride + (pos % a.pool.page_size) * a.pool.slot_stride;
+  const int half = a.hd >> 1, per_head = half >> 2, hkv = a.pool.n_kv_heads;
+  const int units = (a.hq + 2 * hkv) * per_head;
+  const float *src = a.qkv + r * a.qkv_stride;
+  for (int u = blockIdx.y * 256 + threadIdx.x; u < units; u += gridDim.y * 256) {
+    const int h = u / per_head, i = (u - h * per_head) << 2;
+    const bool is_q = h < a.hq, is_k = !is_q && h < a.hq + hkv;
+    if (!is_q && page < 0) continue;
+    const float4 x = *reinterpret_cast<const float4 *>(src + h * a.hd + i), y = *reinterpret_cast<const float4 *>(src + h * a.hd + half + i);
+    float v0[4] = {x.x, x.y, x.z, x.w}, v1[4] = {y.x, y.y, y.z, y.w};
+    if (is_q || is_k) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const double t = (double)pos * a.turns[i + k];
+        float sn, cs;
+        sincospif((float)(2.0 * (t - rint(t))), &sn, &cs);
+        const float o0 = v0[k] * cs - v1[k] * sn, o1 = v0[k] * sn + v1[k] * cs;
+        v0[k] = o0; v1[k] = o1;
+      }
+    }
+    T *dst = is_q ? (T *)a.q + ((long long)r * a.hq + h) * a.hd
+                  : (T *)(is_k ? a.pool.k : a.pool.v) + slot + (long long)(h - a.hq - (is_k ? 0 : hkv)) * a.pool.head_stride;
+    put4(dst + i, v0);
+    put4(dst + half + i, v1);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+struct PagedAttnArgs {
+  PageView pool;
+  const int32_t *table; int width;
+  const int32_t *kv_len;
+  const void *q; long long q_stride;
+  float *out;
+  int c, hq, window, n_sink;
+};
+
+template <typename T> __device__ __forceinline__ float as_float(T v) { return (float)v; }
+
+// One block per row and query head, its warps take turns at the keys, a lane holds HD / 32 elements.
+template <typename T, int HD>
+__global__ void __launch_bounds__(128) paged_attn_kernel(const __grid_constant__ PagedAttnArgs a) {
+  constexpr int E = HD / 32;
+  const int r = blockIdx.x, h = blockIdx.y, b = r / a.c, kvh = h / (a.hq / a.pool.n_kv_heads);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cap = a.width * a.pool.page_size, len = clamp_len(a.kv_len[b], cap);
+  const int p = len + (r - b * a.c);
+  __shared__ float part[4][HD + 2];
+  float q[E], o[E], m = -INFINITY, l = 0.f;
+  const T *qr = (const T *)a.q + r * a.q_stride + h * HD + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) { q[e] = as_float(qr[e]) * rsqrtf((float)HD); o[e] = 0.f; }
+  const int32_t *row = a.table + (long long)b * a.width;
+  const int first = len < 0 ? 0 : window_first(p, a.window), sinks = len < 0 ? 0 : min(a.n_sink, first);
+  const int n = len < 0 ? 0 : sinks + p + 1 - first;
+  for (int i = warp; i < n; i += 4) {
+    const int t = i < sinks ? i : first + i - sinks;
+    const int page = page_of(row, a.width, t, a.pool.page_size, a.pool.n_pages);
+    const long long at = (long long)page * a.pool.page_stride + kvh * a.pool.head_stride + (t % a.pool.page_size) * a.pool.slot_stride + lane * E;
+    float s = 0.f, v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      s = fmaf(q[e], page < 0 ? NAN : as_float(((const T *)a.pool.k)[at + e]), s);
+      v[e] = page < 0 ? NAN : as_float(((const T *)a.pool.v)[at + e]);
+    }
+#pragma unroll
+    for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);
+    const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : expf(m - mn), w = expf(s - mn);
+    l = l * f + w;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = o[e] * f + w * v[e];
+    m = mn;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) part[warp][lane * E + e] = o[e];
+  if (lane == 0) { part[warp][HD] = m; part[warp][HD + 1] = l; }
+  __syncthreads();
+  for (int e = threadIdx.x; e < HD; e += 128) {
+    float M = -INFINITY, den = 0.f, sum = 0.f;
+    for (int w = 0; w < 4; ++w) M = fmaxf(M, part[w][HD]);
+    for (int w = 0; w < 4; ++w) {
+      const float f = part[w][HD] == -INFINITY && part[w][HD + 1] == 0.f ? 0.f : expf(part[w][HD] - M);
+      den += f * part[w][HD + 1];
+      sum += f * part[w][e];
+    }
+    a.out[((long long)r * a.hq + h) * HD + e] = den == 0.f ? 0.f : sum / den;
+  }
+}
+
+template <typename T>
+cudaError_t launch_paged_attn(const PagedAttnArgs &a, int hd, int batch, cudaStream_t st) {
+  const dim3 grid(batch * a.c, a.hq);
+  if (hd == 128) paged_attn_kernel<T, 128><<<grid, 128, 0, st>>>(a);
+  else if (hd == 64) paged_attn_kernel<T, 64><<<grid, 128, 0, st>>>(a);
+  else paged_attn_kernel<T, 32><<<grid, 128, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------------ arguments
+int call_ok(const fc_pages *pages, int layer, const int32_t *table, int width, const int32_t *kv_len, int batch, int c, int hq) {
+  if (int rc = pages_ok(pages)) return rc;
+  if (!table || !kv_len || layer < 0 || layer >= pages->n_layers || width < 1 || batch < 1 || c < 1 || c > 64 || hq < 1) return FC_ERR_ARG;
+  if (hq % pages->n_kv_heads) return FC_ERR_ARG;
+  if ((long long)width * pages->page_size > INT_MAX - 1024 || (long long)batch * c > INT_MAX / 2 || hq > 65535) return FC_ERR_CAPACITY;
+  return FC_OK;
+}
+
+PageView view_of(const fc_pages *p, int layer) {
+  PageView v;
+  const long long off = layer * p->layer_stride * (p->dtype == FC_F32 ? 4 : 2);
+  v.k = (char *)p->k + off; v.v = (char *)p->v + off;
+  v.page_stride = p->page_stride; v.head_stride = p->head_stride; v.slot_stride = p->slot_stride;
+  v.n_pages = p->n_pages; v.page_size = p->page_size; v.n_kv_heads = p->n_kv_heads;
+  return v;
+}
+
+}  // namespace
+}  // namespace fc
+
+using namespace fc;
+
+extern "C" int fc_op_paged_store(const fc_pages *pages, int32_t layer, const int32_t *table, int32_t table_width, const int32_t *kv_len,
+                                 const float *qkv, int64_t qkv_stride, void *q_out, int32_t batch, int32_t c, int32_t n_heads,
+                                 float rope_theta, void *cuda_stream) {
+  if (int rc = call_ok(pages, layer, table, table_width, kv_len, batch, c, n_heads)) return rc;
+  const int hd = pages->head_dim;
+  if (!qkv || !q_out || ((uintptr_t)qkv | (uintptr_t)q_out) % 16 || qkv_stride % 4 ||
+      qkv_stride < (int64_t)(n_heads + 2 * pages->n_kv_heads) * hd || !(rope_theta > 0.f) || std::isinf(rope_theta)) return FC_ERR_ARG;
+  PagedStoreArgs a;
+  a.pool = view_of(pages, layer);
+  a.table = table; a.width = table_width; a.kv_len = kv_len; a.qkv = qkv; a.qkv_stride = qkv_stride; a.q = q_out;
+  a.c = c; a.hq = n_heads; a.hd = hd;
+  for (int i = 0; i < hd / 2; ++i) a.turns[i] = std::pow((double)rope_theta, -2.0 * i / hd) / 6.283185307179586476925286766559;
+  const int rows = batch * c, units = (n_heads + 2 * pages->n_kv_heads) * (hd >> 3);
+  int ny = (4 * 148 + rows - 1) / rows;               // about four blocks per SM when there are few rows
+  if (ny > (units + 255) / 256) ny = (units + 255) / 256;
+  const dim3 grid(rows, ny);
+  if (pages->dtype == FC_F32) paged_store_kernel<float><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+  else paged_store_kernel<__nv_bfloat16><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+  return cudaGetLastError() == cudaSuccess ? FC_OK : FC_ERR_CUDA;
+}
+
+extern "C" size_t fc_op_paged_attention_scratch_bytes(int32_t batch, int32_t c, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                      int32_t dtype) {
+  if (batch < 1 || c < 1 || c > 64 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return 0;
+  if ((head_dim != 32 && head_dim != 64 && head_dim != 128) || (dtype != FC_F32 && dtype != FC_BF16)) return 0;
+  return 256;
+}
+
+extern "C" int fc_op_paged_attention(const fc_pages *pages, int32_t layer, const int32_t *table, int32_t table_width, const int32_t *kv_len,
+                                     const void *q, int64_t q_stride, float *out, int32_t batch, int32_t c, int32_t n_heads,
+                                     int32_t window, int32_t n_sink, void *scratch, size_t scratch_bytes, void *cuda_stream) {
+  if (int rc = call_ok(pages, layer, table, table_width, kv_len, batch, c, n_heads)) return rc;
+  const int hd = pages->head_dim, per = pages->dtype == FC_F32 ? 4 : 8;
+  if (!q || !out || !scratch || ((uintptr_t)q | (uintptr_t)out) % 16 || (uintptr_t)scratch % 256 || q_stride % per ||
+      q_stride < (int64_t)n_heads * hd || window < 0 || n_sink < 0) return FC_ERR_ARG;
+  if (scratch_bytes < fc_op_paged_attention_scratch_bytes(batch, c, n_heads, pages->n_kv_heads, hd, pages->dtype)) return FC_ERR_CAPACITY;
+  PagedAttnArgs a;
+  a.pool = view_of(pages, layer);
+  a.table = table; a.width = table_width; a.kv_len = kv_len; a.q = q; a.q_stride = q_stride; a.out = out;
+  a.c = c; a.hq = n_heads; a.window = window; a.n_sink = n_sink;
+  const cudaError_t e = pages->dtype == FC_F32 ? launch_paged_attn<float>(a, hd, batch, (cudaStream_t)cuda_stream)
+                                               : launch_paged_attn<__nv_bfloat16>(a, hd, batch, (cudaStream_t)cuda_stream);
+  return e == cudaSuccess ? FC_OK : FC_ERR_CUDA;
+}

@@ -28,7 +28,9 @@ EXPORTS = ["fc_kv_bytes", "fc_workspace_bytes", "fc_init", "fc_prefill", "fc_jac
            "fc_last_launch_count", "fc_last_route", "fc_destroy", "fc_strerror", "fc_last_cuda_error",
            "fc_op_linear", "fc_op_accept", "fc_op_window_attention",
            "fc_op_window_attention_scratch_bytes", "fc_op_window_attention_noalloc",
-           "fc_op_fused_window_attention", "fc_op_short_window_attention", "fc_op_fused_window_attention_scratch_bytes"]
+           "fc_op_fused_window_attention", "fc_op_short_window_attention", "fc_op_fused_window_attention_scratch_bytes",
+           "fc_op_paged_store", "fc_op_paged_attention", "fc_op_paged_attention_scratch_bytes", "fc_op_pages_fork", "fc_op_pages_free",
+           "fc_op_pages_reserve", "fc_op_pages_reserve_scratch_bytes", "fc_op_pages_compact", "fc_op_pages_compact_scratch_bytes"]
 
 
 class fc_model_shape(C.Structure):
@@ -51,6 +53,12 @@ class fc_weights(C.Structure):
 class fc_stats(C.Structure):
     _fields_ = [("steps", C.c_int64), ("tokens", C.c_int64), ("accept_hist", C.c_int32 * 65),
                 ("ms_prefill", C.c_float), ("ms_steps", C.c_float)]
+
+
+class fc_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("dtype", "n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim")] + \
+               [(n, C.c_int64) for n in ("layer_stride", "page_stride", "head_stride", "slot_stride")]
 
 
 _lib = None
@@ -106,5 +114,18 @@ def load() -> C.CDLL:
                                                 [vp, C.c_size_t, vp]
     lib.fc_op_short_window_attention.argtypes = [vp, vp, C.c_float, i32, C.c_float, vp, vp, vp, vp] + [i32] * 7 + \
                                                 [vp, C.c_size_t, vp]
+    i64, pg = C.c_int64, C.POINTER(fc_pages)
+    lib.fc_op_paged_store.argtypes = [pg, i32, vp, i32, vp, vp, i64, vp, i32, i32, i32, C.c_float, vp]
+    lib.fc_op_paged_attention_scratch_bytes.restype = C.c_size_t
+    lib.fc_op_paged_attention_scratch_bytes.argtypes = [i32] * 6
+    lib.fc_op_paged_attention.argtypes = [pg, i32, vp, i32, vp, vp, i64, vp] + [i32] * 5 + [vp, C.c_size_t, vp]
+    lib.fc_op_pages_fork.argtypes = [vp, i32, i32, vp, vp, i32, i32, vp, vp, i32, vp]
+    lib.fc_op_pages_free.argtypes = [vp, i32, i32, vp, vp, i32, i32, vp, i32, i32, i32, vp]
+    lib.fc_op_pages_reserve_scratch_bytes.restype = C.c_size_t
+    lib.fc_op_pages_reserve_scratch_bytes.argtypes = [i32] * 2
+    lib.fc_op_pages_reserve.argtypes = [pg, vp, i32, i32, vp, vp, i32, vp, vp, C.c_size_t, vp]
+    lib.fc_op_pages_compact_scratch_bytes.restype = C.c_size_t
+    lib.fc_op_pages_compact_scratch_bytes.argtypes = [i32]
+    lib.fc_op_pages_compact.argtypes = [pg, vp, i32, i32, vp, vp, vp, C.c_size_t, vp]
     _lib = lib
     return lib

@@ -1,0 +1,540 @@
+"""The paged K/V cache on the GPU against plain Python in 64 bits: rotation and write, attention with and without a sliding window, and
+what manages the pages.  Slots that nobody should read hold NaN."""
+import math
+import random
+
+import pytest
+import torch
+
+import paged_reference as ref
+from paper_2311_08263_b200 import engine, lib
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _pools(n_pages, hkv, ps, hd, dtype, order="hnd", fill=math.nan):
+    """K and V [pages, kv heads, slots, hd] in one of the layouts: hnd, nhd, K and V taking turns page by page, padded rows."""
+    if order == "hnd":
+        return [torch.full((n_pages, hkv, ps, hd), fill, dtype=dtype, device="cuda") for _ in range(2)]
+    if order == "nhd":
+        return [torch.full((n_pages, ps, hkv, hd), fill, dtype=dtype, device="cuda").transpose(1, 2) for _ in range(2)]
+    if order == "turns":
+        both = torch.full((n_pages, 2, hkv, ps, hd), fill, dtype=dtype, device="cuda")
+        return [both[:, 0], both[:, 1]]
+    assert order == "padded"
+    return [torch.full((n_pages + 1, hkv, ps + 1, hd + 8), fill, dtype=dtype, device="cuda")[1:, :, 1:, 8:] for _ in range(2)]
+
+
+def _dealt(lens, c, ps, gen, extra=2):
+    """A table with slots for lens[b] + c positions, pages in random order, -1 elsewhere; pages of the pool."""
+    need = [-(-(n + c) // ps) if n >= 0 else 0 for n in lens]
+    ids = torch.randperm(sum(need) + extra, generator=gen).tolist()
+    table = torch.full((len(lens), max(max(need), 1) + 1), -1, dtype=torch.int32)
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = torch.tensor(ids[at:at + n], dtype=torch.int32)
+        at += n
+    return table, len(ids)
+
+
+def _cache(lens, c, hkv, hd, ps, dtype, order, seed, window=0, n_sink=0):
+    """Pools in which only the slots that some row sees hold numbers; table, lengths."""
+    gen = torch.Generator().manual_seed(seed)
+    table, n_pages = _dealt(lens, c, ps, gen)
+    k, v = _pools(n_pages, hkv, ps, hd, dtype, order)
+    for b, n in enumerate(lens):
+        if n < 0:
+            continue
+        t = sorted({i for j in range(c) for i in ref.visible(n + j, window, n_sink)})
+        page, slot = table[b, [i // ps for i in t]].long().cuda(), torch.tensor([i % ps for i in t]).cuda()
+        for x in (k, v):
+            x[page, :, slot] = torch.randn(len(t), hkv, hd, generator=gen).to(dtype).cuda()
+    return k, v, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+
+
+def _queries(n, width, dtype, seed):
+    return (1.5 * torch.randn(n, width, generator=torch.Generator().manual_seed(seed))).to(dtype).cuda()
+
+
+def _close(got, want, tol):
+    got = got.double().cpu().view_as(want)
+    assert torch.equal(got.isnan(), want.isnan())
+    fine = ~want.isnan()
+    off = ((got - want).abs() - tol)[fine]
+    assert off.numel() == 0 or off.max() <= 1e-30, (off.max(), (got - want).abs()[fine].max())
+
+
+# ---------------------------------------------------------------------------------------------------------------- store
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,hkv,hd,ps,order,c", [
+    (4, 4, 32, 16, "hnd", 8), (8, 2, 64, 5, "nhd", 1), (8, 8, 128, 1, "turns", 3), (6, 2, 128, 16, "padded", 64), (32, 4, 64, 64, "hnd", 2)])
+def test_store(dtype, hq, hkv, hd, ps, order, c):
+    lens = [0, 7, -1, 130, 63, 64]
+    gen = torch.Generator().manual_seed(hd + ps)
+    table, n_pages = _dealt(lens, c, ps, gen)
+    table[4, lens[4] // ps] = -1                                             # a page that is missing
+    table[5, lens[5] // ps] = n_pages                                        # and one beyond the pool
+    k, v = _pools(n_pages, hkv, ps, hd, DT[dtype], order, 7.0)
+    wide = torch.randn(len(lens) * c, (hq + 2 * hkv) * hd + 4, generator=gen).cuda()
+    qkv = wide[:, 4:]
+    theta = 10000.0
+    q = engine.fc_op_paged_store(qkv, k, v, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), c, hq, theta)
+    x = qkv.double().cpu().view(len(lens), c, -1, hd)
+    want_k, want_v = torch.full((n_pages, hkv, ps, hd), 7.0, dtype=torch.float64), torch.full((n_pages, hkv, ps, hd), 7.0, dtype=torch.float64)
+    # a rotated element is two products and a sum of rounded factors: the angle's fraction rounded once (half a step of up to a half turn, times
+    # pi), sine and cosine off by 2 steps; then the type's own rounding
+    for b, n in enumerate(lens):
+        if n < 0:
+            continue
+        rot = ref.rotated(x[b], range(n, n + c), theta)
+        size = x[b].abs()[..., :hd // 2] + x[b].abs()[..., hd // 2:]
+        size = torch.cat([size, size], -1)
+        half = torch.finfo(DT[dtype]).eps / 2
+        tol = size * (math.pi * 2 ** -24 + 6 * 2.0 ** -24) + (rot.abs() + size * 1e-6) * half
+        got = q.view(len(lens), c, hq, hd)[b].double().cpu()
+        assert ((got - rot[:, :hq]).abs() <= tol[:, :hq]).all()
+        for j in range(c):
+            page = int(table[b, (n + j) // ps])
+            if 0 <= page < n_pages:
+                want_k[page, :, (n + j) % ps], want_v[page, :, (n + j) % ps] = rot[j, hq:hq + hkv], x[b, j, hq + hkv:]
+                at = (page, slice(None), (n + j) % ps)
+                assert ((k[at].double().cpu() - rot[j, hq:hq + hkv]).abs() <= tol[j, hq:hq + hkv]).all()
+                assert torch.equal(v[at].cpu(), qkv.view(len(lens), c, -1, hd)[b, j, hq + hkv:].cpu().to(DT[dtype]))
+    untouched = want_k == 7.0
+    assert (k.double().cpu()[untouched] == 7.0).all() and (v.double().cpu()[want_v == 7.0] == 7.0).all()
+
+
+def test_store_far_positions():
+    """Positions whose angle a 32-bit product would miss by whole radians."""
+    hd, n = 128, 2 ** 30 + 12345
+    k, v = _pools(2, 1, 1 << 16, hd, torch.float32, fill=0.0)
+    width = n // (1 << 16) + 2
+    table = torch.full((1, width), -1, dtype=torch.int32)
+    table[0, n // (1 << 16)] = 1
+    x = torch.randn(2, 3 * hd, generator=torch.Generator().manual_seed(1))
+    q = engine.fc_op_paged_store(x.cuda(), k, v, table.cuda(), torch.tensor([n], dtype=torch.int32).cuda(), 2, 1, 1e6)
+    want = ref.rotated(x.double().view(2, 3, hd)[:, :1], [n, n + 1], 1e6)
+    # a 64-bit product of 2^30 turns is off by 2^-53 x 2^28, and so is the reference's angle
+    assert (q.double().cpu().view(2, 1, hd) - want).abs().max() < 4 * (2 ** -24 * 8 + 2 ** -22)
+    slot = n % (1 << 16)
+    assert torch.equal(v[1, 0, slot].cpu(), x[0, 2 * hd:]) and torch.equal(v[1, 0, slot + 1].cpu(), x[1, 2 * hd:])
+
+
+# ---------------------------------------------------------------------------------------------------------------- attention
+EDGES = [0, 1, 7, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, -1, 260]
+ATTENTION = [
+    # hq, hkv, hd, c, page, layout, lens, window, sinks
+    (4, 4, 32, 8, 16, "hnd", [70], 0, 0),
+    (4, 4, 32, 1, 16, "hnd", EDGES, 0, 0),
+    (8, 2, 64, 1, 16, "nhd", EDGES, 0, 0),
+    (8, 8, 128, 1, 32, "turns", EDGES, 0, 0),
+    (8, 1, 64, 5, 24, "padded", EDGES, 0, 0),
+    (8, 8, 128, 16, 16, "hnd", [803], 0, 0),
+    (32, 4, 64, 16, 64, "hnd", [300, 0, 129], 0, 0),                         # 128 queries per kv head
+    (4, 2, 128, 64, 48, "nhd", [200, 1, -1, 77], 0, 0),
+    (5, 5, 64, 3, 1, "hnd", [40, 2, 0], 0, 0),                               # a slot per page
+    (6, 2, 128, 2, 1000, "hnd", [999, 998, 1000], 0, 0),                     # a sequence per page
+    (16, 1, 128, 7, 5, "hnd", [333, 5, 64], 0, 0),                           # 112 queries on one kv head, pages that end inside tiles
+    (4, 4, 32, 3, 16, "hnd", EDGES, 1, 0),
+    (8, 2, 64, 4, 16, "nhd", EDGES, 20, 4),
+    (8, 8, 128, 1, 16, "hnd", [500, 90, 3], 64, 1),
+    (4, 1, 128, 16, 8, "hnd", [700, 250], 100, 200),                         # sinks that reach past the window's start in one of them
+    (8, 2, 64, 64, 32, "hnd", [400, 10], 33, 5),
+    (2, 2, 64, 1, 64, "hnd", [9000], 0, 0),                                  # two heads: split over the length
+    (2, 1, 128, 2, 16, "hnd", [5000, 0, 3], 4096, 16),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", range(len(ATTENTION)))
+def test_attention(dtype, case):
+    hq, hkv, hd, c, ps, order, lens, window, n_sink = ATTENTION[case]
+    k, v, table, kv_len = _cache(lens, c, hkv, hd, ps, DT[dtype], order, 100 + case, window, n_sink)
+    wide = _queries(len(lens) * c, hq * hd + 8, DT[dtype], case)
+    for q in (wide[:, 8:], wide[:, 8:].contiguous()):
+        out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq, window=window, n_sink=n_sink)
+        _close(out, *ref.attention(q, k, v, table, kv_len, c, hq, window, n_sink))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("seed", range(24))
+def test_attention_random_shapes(dtype, seed):
+    r = random.Random(seed)
+    hkv, group, hd = r.choice([1, 2, 3]), r.choice([1, 2, 3, 8, 13]), r.choice([32, 64, 128])
+    c, ps, B = r.choice([1, 1, 2, 5, 16, 33, 64]), r.choice([1, 3, 8, 16, 20, 64, 128]), r.randint(1, 5)
+    lens = [r.choice([-1, 0, 1, r.randint(2, 60), r.randint(60, 500)]) for _ in range(B)]
+    window = r.choice([0, 0, 1, r.randint(2, 40), r.randint(40, 300)])
+    n_sink = r.choice([0, 1, 5, 40])
+    k, v, table, kv_len = _cache(lens, c, hkv, hd, ps, DT[dtype], r.choice(["hnd", "nhd", "turns", "padded"]), seed, window, n_sink)
+    q = _queries(B * c, hkv * group * hd, DT[dtype], seed)
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hkv * group, window=window, n_sink=n_sink)
+    _close(out, *ref.attention(q, k, v, table, kv_len, c, hkv * group, window, n_sink))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (6, 2)])
+def test_later_rows_do_not_reach_earlier_ones(dtype, window, n_sink):
+    """Infinities and NaN in the window's later keys and values: rows that do not see them stay as they are, bit for bit."""
+    hq, hkv, hd, c, ps, lens = 8, 2, 64, 12, 16, [50, 3, 0]
+    k, v, table, kv_len = _cache(lens, c, hkv, hd, ps, DT[dtype], "hnd", 5, window, n_sink)
+    q = _queries(len(lens) * c, hq * hd, DT[dtype], 6)
+    good = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq, window=window, n_sink=n_sink).view(len(lens), c, hq, hd)
+    for bad in (math.nan, math.inf, -math.inf):
+        for at in (4, 11):
+            k2, v2 = k.clone(), v.clone()
+            for b, n in enumerate(lens):
+                page, slot = int(table[b, (n + at) // ps]), (n + at) % ps
+                v2[page, :, slot, ::3] = bad
+                if bad != bad:
+                    k2[page, :, slot, 5] = bad
+            out = engine.fc_op_paged_attention(q, k2, v2, table, kv_len, c, hq, window=window, n_sink=n_sink).view(len(lens), c, hq, hd)
+            for j in range(c):
+                sees = [at + n in ref.visible(n + j, window, n_sink) for n in lens]
+                for b in range(len(lens)):
+                    if not sees[b]:
+                        assert torch.equal(out[b, j], good[b, j]), (b, j)
+                    elif bad != bad:
+                        assert out[b, j].isnan().all()
+                    else:
+                        assert (out[b, j, :, ::3] == bad).all() and out[b, j, :, 1::3].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bad_pages_reach_only_the_rows_that_see_them(dtype):
+    hq, hkv, hd, c, ps, lens = 4, 2, 128, 4, 16, [100, 100, 100, 40]
+    k, v, table, kv_len = _cache(lens, c, hkv, hd, ps, DT[dtype], "hnd", 8, 40, 2)
+    table[0, 2:3] = -1                                                       # positions 32..47: no row sees them
+    table[1, 5] = k.shape[0]                                                 # beyond the pool, seen by all rows
+    table[2, 6] = 2 ** 31 - 1                                                # the window's own page: positions 96..111
+    table[3, 2] = -5                                                         # positions 32..47
+    q = _queries(len(lens) * c, hq * hd, DT[dtype], 6)
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq, window=40, n_sink=2)
+    _close(out, *ref.attention(q, k, v, table, kv_len, c, hq, 40, 2))
+    assert out.view(4, -1)[0].isfinite().all() and all(out.view(4, -1)[b].isnan().all() for b in (1, 2, 3))
+    # a table that is too short: the rows at positions beyond it
+    short = table[3:4, :2].contiguous()
+    short[0, 1] = table[3, 1]
+    for n in (28, 29, 31, 32, 2 ** 31 - 1):
+        lens1 = torch.tensor([n], dtype=torch.int32).cuda()
+        k[:], v[:] = 0.5, 0.25
+        out = engine.fc_op_paged_attention(q[:c], k, v, short, lens1, c, hq)
+        for j in range(c):
+            assert out[j].isnan().all() if n + j >= 32 else torch.equal(out[j], torch.full_like(out[j], 0.25))
+
+
+def test_table_without_sequences():
+    k, v = _pools(3, 2, 16, 64, torch.bfloat16)
+    table = torch.full((5, 4), -1, dtype=torch.int32).cuda()
+    q = _queries(10, 4 * 64, torch.bfloat16, 0)
+    out = engine.fc_op_paged_attention(q, k, v, table, torch.full((5,), -1, dtype=torch.int32).cuda(), 2, 4)
+    assert torch.equal(out, torch.zeros_like(out))
+
+
+def test_one_visible_key_is_its_value():
+    k, v, table, kv_len = _cache([0, 0], 1, 3, 64, 16, torch.bfloat16, "hnd", 3)
+    out = engine.fc_op_paged_attention(_queries(2, 6 * 64, torch.bfloat16, 0), k, v, table, kv_len, 1, 6)
+    want = v[table[:, 0].long(), :, 0].float().repeat_interleave(2, 1).view(2, -1)
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_scores(dtype):
+    """Scores of some thousands: the running maximum keeps the exponentials in range; what is far below it counts as nothing."""
+    hq, hkv, hd, c, ps = 2, 2, 128, 2, 16
+    k, v, table, kv_len = _cache([300], c, hkv, hd, ps, DT[dtype], "hnd", 3)
+    q = _queries(c, hq * hd, DT[dtype], 1) * 300
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq)
+    _close(out, *ref.attention(q, k, v, table, kv_len, c, hq))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_offsets_beyond_32_bits(dtype):
+    """Pages that lie more than 2^32 bytes and 2^31 elements into the pool."""
+    hkv, hd, ps, hq = 8, 128, 64, 8
+    n_pages = 2 ** 31 // (hkv * hd * ps) + 40
+    k, v = (torch.empty(n_pages, hkv, ps, hd, dtype=DT[dtype], device="cuda") for _ in range(2))
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 3, n_pages - 2]], dtype=torch.int32).cuda()
+    for x in (k, v):
+        for p in table[0].tolist():
+            x[p] = torch.randn(hkv, ps, hd, generator=torch.Generator().manual_seed(p)).to(DT[dtype]).cuda()
+    n = 200
+    qkv = torch.randn(1, 3 * hq * hd, generator=torch.Generator().manual_seed(2)).cuda()
+    kv_len = torch.tensor([n], dtype=torch.int32).cuda()
+    q = engine.fc_op_paged_store(qkv, k, v, table, kv_len, 1, hq, 1e4)
+    assert torch.equal(v[n_pages - 2, :, n - 192].cpu(), qkv[0, 2 * hq * hd:].view(hkv, hd).cpu().to(DT[dtype]))
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, 1, hq)
+    few = table[0].long()
+    _close(out, *ref.attention(q, k[few], v[few], torch.tensor([[0, 1, 2, 3]]), kv_len, 1, hq))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_slab_of_a_context_is_a_pool(dtype):
+    """One page of max_seq slots per sequence: the same as fc_op_window_attention over the slab."""
+    B, hkv, max_seq, hd, hq, c = 3, 2, 200, 64, 8, 4
+    gen = torch.Generator().manual_seed(4)
+    k, v = (torch.randn(B, hkv, max_seq, hd, generator=gen).to(DT[dtype]).cuda() for _ in range(2))
+    kv_len = torch.tensor([150, 0, 196], dtype=torch.int32).cuda()
+    q = _queries(B * c, hq * hd, DT[dtype], 4)
+    table = torch.arange(B, dtype=torch.int32).cuda().view(B, 1)
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq)
+    want, tol = ref.attention(q, k, v, table, kv_len, c, hq)
+    _close(out, want, tol)
+    slab = engine.fc_op_window_attention(q, k, v, kv_len, c, hq, 196)
+    # that kernel's own error is of the same kind; its probabilities are one bf16 pair as well
+    _close(slab, want, 2 * tol + 1e-6)
+
+
+def test_repeated_and_concurrent_calls_give_the_same_bits():
+    cases = []
+    for i, (hq, hkv, hd, c, lens, window) in enumerate([(32, 4, 64, 1, [5000], 0), (8, 8, 128, 16, [803, 20], 0), (16, 2, 64, 16, [900, 31, 2], 300)]):
+        k, v, table, kv_len = _cache(lens, c, hkv, hd, 16, torch.bfloat16, "hnd", i, window, 3)
+        cases.append((_queries(len(lens) * c, hq * hd, torch.bfloat16, i), k, v, table, kv_len, c, hq, window, 3))
+    first = [engine.fc_op_paged_attention(*a) for a in cases]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for s, a in zip(streams, cases):
+            with torch.cuda.stream(s):
+                got.append(engine.fc_op_paged_attention(*a))
+    torch.cuda.synchronize()
+    for i, x in enumerate(got):
+        assert torch.equal(x, first[i % 3])
+
+
+# ---------------------------------------------------------------------------------------------------------------- pages
+class _Both:
+    """The device's pool and its model in Python, compared after every operation."""
+
+    def __init__(self, n_pages, n_seqs, width, ps, order="hnd", dtype=torch.bfloat16, layers=3, hkv=2, hd=64):
+        self.model = ref.Pool(n_pages, n_seqs, width, ps)
+        # every page of every layer is filled with one number of its own
+        self.k, self.v = (torch.stack([x for _ in range(layers)]) for x in _pools(n_pages, hkv, ps, hd, dtype, order))
+        if order == "nhd":
+            self.k, self.v = (torch.empty(layers, n_pages, ps, hkv, hd, dtype=dtype, device="cuda").transpose(2, 3) for _ in range(2))
+        if order == "padded":
+            self.k, self.v = (torch.full((layers, n_pages, hkv, ps + 3, hd + 8), 9.0, dtype=dtype, device="cuda")[:, :, :, 1:-2, 8:] for _ in range(2))
+        if order == "turns":
+            both = torch.empty(n_pages, layers, 2, hkv, ps, hd, dtype=dtype, device="cuda")
+            self.k, self.v = both[:, :, 0].transpose(0, 1), both[:, :, 1].transpose(0, 1)
+        mark = torch.arange(n_pages, dtype=torch.float32).view(1, -1, 1, 1, 1)
+        lay = torch.arange(layers, dtype=torch.float32).view(-1, 1, 1, 1, 1)
+        slot = torch.arange(ps, dtype=torch.float32).view(1, 1, 1, -1, 1) % 2
+        self.want = lambda m, sign: (sign * (torch.tensor(m, dtype=torch.float32).view(1, -1, 1, 1, 1) + 64 * lay + 0.5 * slot)).expand(
+            layers, len(m), hkv, ps, hd).to(dtype)
+        for x, sign in ((self.k, 1), (self.v, -1)):
+            x.copy_(self.want(list(range(n_pages)), sign).cuda())
+        self.table = torch.full((n_seqs, width), -1, dtype=torch.int32).cuda()
+        self.kv_len = torch.full((n_seqs,), -1, dtype=torch.int32).cuda()
+        self.refs = torch.zeros(n_pages, dtype=torch.int32).cuda()
+
+    def check(self):
+        m = self.model
+        assert self.table.tolist() == m.table and self.kv_len.tolist() == m.kv_len and self.refs.tolist() == m.refs
+        held = [p for p, r in enumerate(m.refs) if r > 0]                     # what free pages hold means nothing
+        for x, sign in ((self.k, 1), (self.v, -1)):
+            assert torch.equal(x[:, held].cpu(), self.want([m.content[p] for p in held], sign))
+        counts = [0] * len(m.refs)
+        for row in m.table:
+            for p in row:
+                if p >= 0:
+                    counts[p] += 1
+        assert counts == m.refs
+
+    def start(self, s, n):
+        self.kv_len[s] = self.model.kv_len[s] = n
+
+    grow = start
+
+    def free(self, seqs, window=0, n_sink=0):
+        self.model.free(seqs, window, n_sink)
+        engine.fc_op_pages_free(self.table, self.kv_len, self.refs, self.model.ps, seqs, window, n_sink)
+
+    def fork(self, src, dst):
+        self.model.fork(src, dst)
+        engine.fc_op_pages_fork(self.table, self.kv_len, self.refs, self.model.ps, src, dst)
+
+    def reserve(self, rows):
+        want = self.model.reserve(rows)
+        got = engine.fc_op_pages_reserve(self.k, self.v, self.table, self.kv_len, self.refs, rows).tolist()
+        assert got == want
+        return want
+
+    def compact(self):
+        want = self.model.compact()
+        assert engine.fc_op_pages_compact(self.k, self.v, self.table, self.refs).tolist() == [want]
+        self.model.content = list(self.model.content)
+
+
+@pytest.mark.parametrize("order", ["hnd", "nhd", "padded", "turns"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_fork_and_copy_on_write(order, dtype):
+    p = _Both(40, 6, 8, 5, order, DT[dtype])
+    p.start(0, 0)
+    p.reserve(13)                                                            # pages 0..2
+    p.grow(0, 13)
+    p.fork([0, 0, 0], [1, 2, 4])
+    p.check()
+    assert p.model.refs[:3] == [4, 4, 4]
+    assert p.reserve(4) == [1, 1, 1, 0, 1, 0]                                # three copies of page 2, the last sequence keeps it
+    p.check()
+    assert p.model.table[4][2] == 2 and p.model.refs[:3] == [4, 4, 1]
+    p.free([0, 1])
+    p.check()
+    p.fork([2], [4])                                                         # 4 gives up what it held
+    p.check()
+    p.free([2, 4])
+    p.check()
+    assert sum(p.model.refs) == 0
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_random_lives_of_sequences(seed):
+    r = random.Random(seed)
+    n_seqs, width, ps = r.choice([3, 9, 40]), r.choice([4, 9]), r.choice([1, 3, 8])
+    p = _Both(r.choice([12, 30, 64]), n_seqs, width, ps, r.choice(["hnd", "nhd", "padded", "turns"]), layers=2, hkv=1, hd=32)
+    for _ in range(40):
+        what = r.choice(["start", "fork", "reserve", "reserve", "reserve", "free", "window", "compact"])
+        used = [s for s in range(n_seqs) if p.model.kv_len[s] >= 0]
+        if what == "start" and len(used) < n_seqs:
+            p.start(r.choice([s for s in range(n_seqs) if s not in used]), 0)
+        elif what == "fork" and used and n_seqs > 1:
+            dst = r.sample(range(n_seqs), r.randint(1, min(3, n_seqs - 1)))
+            src = [s for s in range(n_seqs) if s not in dst]
+            p.fork([r.choice(src) for _ in dst], dst)
+        elif what == "reserve":
+            rows = r.choice([1, 2, 7, 20])
+            for b, ok in enumerate(p.reserve(rows)):
+                if ok:
+                    p.grow(b, p.model.kv_len[b] + r.randint(0, rows))
+        elif what == "free" and used:
+            p.free(r.sample(used, r.randint(1, len(used))))
+        elif what == "window" and used:
+            p.free(r.sample(used, r.randint(1, len(used))), r.choice([1, 4, 9]), r.choice([0, 1, 4]))
+        elif what == "compact":
+            p.compact()
+        p.check()
+
+
+def test_reserve_serves_in_order_while_pages_last():
+    p = _Both(6, 5, 4, 4)
+    for s, n in ((0, 0), (1, 0), (2, -1), (3, 0), (4, 0)):
+        p.start(s, n)
+    assert p.reserve(8) == [1, 1, 0, 1, 0]                                   # two pages each, six in the pool
+    p.check()
+    assert p.reserve(8) == [1, 1, 0, 1, 0]
+    p.check()
+    p.grow(1, 12)
+    assert p.reserve(8)[1] == 0                                              # beyond the table
+    p.check()
+
+
+def test_many_pages_and_sequences():
+    """More pages, sequences and listed rows than one block has threads."""
+    n = 1500
+    p = _Both(5000, n, 3, 2, layers=1, hkv=1, hd=32)
+    p.start(0, 0)
+    p.reserve(3)
+    p.grow(0, 3)
+    p.fork([0] * (n - 1), list(range(1, n)))
+    p.check()
+    assert sum(p.reserve(2)) == n
+    p.check()
+    p.free(list(range(0, n, 2)))
+    p.check()
+    p.compact()
+    p.check()
+
+
+def test_compact_of_a_compact_pool_and_of_an_empty_one():
+    p = _Both(20, 3, 6, 4)
+    p.compact()
+    p.check()
+    p.start(1, 0)
+    p.reserve(17)
+    p.compact()
+    p.check()
+
+
+# ---------------------------------------------------------------------------------------------------------------- together
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_questions_behind_one_prompt(dtype):
+    """A prompt cached once and forked, windows of rows stored, some accepted, a sliding window whose old pages are freed, compaction in
+    between, the step captured once and replayed as the caches grow: every step as if each sequence had a cache of its own."""
+    hq, hkv, hd, ps, c, layers, window, n_sink, theta = 8, 2, 64, 8, 4, 2, 24, 3, 1e4
+    n_pages, n_seqs, width = 60, 4, 16
+    gen = torch.Generator().manual_seed(9)
+    k, v = (torch.full((layers, n_pages, hkv, ps, hd), math.nan, dtype=DT[dtype], device="cuda") for _ in range(2))
+    table = torch.full((n_seqs, width), -1, dtype=torch.int32).cuda()
+    kv_len = torch.full((n_seqs,), -1, dtype=torch.int32).cuda()
+    refs = torch.zeros(n_pages, dtype=torch.int32).cuda()
+    qkv = torch.zeros(layers, n_seqs * c, (hq + 2 * hkv) * hd).cuda()
+    own = {b: [] for b in range(n_seqs)}                                     # committed rows of each sequence, [layers, width]
+
+    def step():
+        served = engine.fc_op_pages_reserve(k, v, table, kv_len, refs, c)
+        outs = []
+        for i in range(layers):
+            q = engine.fc_op_paged_store(qkv[i], k[i], v[i], table, kv_len, c, hq, theta)
+            outs.append((q, engine.fc_op_paged_attention(q, k[i], v[i], table, kv_len, c, hq, window=window, n_sink=n_sink)))
+        return served, outs
+
+    def check(served, outs):
+        for b in range(n_seqs):
+            n = int(kv_len[b])
+            if n < 0:
+                assert all((o.view(n_seqs, -1)[b] == 0).all() for _, o in outs)
+                continue
+            assert int(served[b]) == 1
+            half = torch.finfo(DT[dtype]).eps / 2
+            seen = sorted({t for j in range(c) for t in ref.visible(n + j, window, n_sink)})
+            page = table[b, [t // ps for t in seen]].long()
+            slot = torch.tensor([t % ps for t in seen]).cuda()
+            for i in range(layers):
+                # what the sequence sees is its own, wherever it lies
+                rows = torch.stack([x[i] for x in own[b]] + list(qkv[i].view(n_seqs, c, -1)[b].cpu())).view(n + c, -1, hd)[seen]
+                rot = ref.rotated(rows[:, hq:hq + hkv].double(), seen, theta)
+                assert ((k[i][page, :, slot].double().cpu() - rot).abs() <= rot.abs() * half + 16 * 2.0 ** -24 * (1 + half)).all()
+                assert torch.equal(v[i][page, :, slot].cpu(), rows[:, hq + hkv:].to(DT[dtype]))
+                want, tol = ref.attention(outs[i][0].view(n_seqs, c, -1)[b], k[i], v[i], table[b:b + 1], kv_len[b:b + 1], c, hq, window, n_sink)
+                _close(outs[i][1].view(n_seqs, c, hq, hd)[b], want, tol)
+
+    kv_len[0] = 0
+    r = random.Random(3)
+
+    def advance(served, outs, most):
+        check(served, outs)
+        lens = kv_len.tolist()
+        for b in range(n_seqs):
+            if lens[b] >= 0:
+                take = r.randint(1, most)
+                own[b] += [qkv[:, b * c + j].cpu() for j in range(take)]
+                kv_len[b] = lens[b] + take
+
+    for _ in range(8):                                                       # the prompt, up to c rows at a time
+        qkv.copy_(torch.randn(qkv.shape, generator=gen))
+        advance(*step(), c)
+    engine.fc_op_pages_fork(table, kv_len, refs, ps, [0, 0], [1, 3])
+    own[1], own[3] = list(own[0]), list(own[0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        kept = step()
+    for i in range(14):
+        qkv.copy_(torch.randn(qkv.shape, generator=gen))
+        graph.replay()
+        advance(*kept, c)
+        if i % 4 == 1:
+            engine.fc_op_pages_free(table, kv_len, refs, ps, [b for b in range(n_seqs) if int(kv_len[b]) >= 0], window, n_sink)
+        if i % 5 == 2:
+            engine.fc_op_pages_compact(k, v, table, refs)
+        if i == 6:
+            engine.fc_op_pages_free(table, kv_len, refs, ps, [1])
+            engine.fc_op_pages_fork(table, kv_len, refs, ps, [3], [2])
+            own[2], own[1] = list(own[3]), []
+    held = table[table >= 0].tolist()
+    assert [held.count(p) for p in range(n_pages)] == refs.tolist()

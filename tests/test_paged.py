@@ -1,0 +1,207 @@
+"""Paged K/V cache without a GPU: calls that are refused before anything is launched, scratch sizes, the index arithmetic of the kernels."""
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+import torch
+
+import paged_reference as ref
+from paper_2311_08263_b200 import build, engine, lib
+
+P = 1 << 20                                  # stands for device pointers: a refused call touches none
+
+
+def _pool(**kw):
+    p = lib.fc_pages(P, 2 * P, lib.FC_BF16, 2, 10, 4, 16, 64, 10 * 4 * 16 * 64, 4 * 16 * 64, 16 * 64, 64)
+    for name, value in kw.items():
+        setattr(p, name, value)
+    return p
+
+
+@pytest.fixture(scope="module")
+def l():
+    build.build()
+    return lib.load()
+
+
+def _store(l, pool=None, layer=0, table=P, width=5, kv_len=P, qkv=P, stride=16 * 64, q=P, batch=3, c=2, hq=8, theta=1e4):
+    return l.fc_op_paged_store(_pool() if pool is None else pool, layer, table, width, kv_len, qkv, stride, q, batch, c, hq, theta, None)
+
+
+def _attention(l, pool=None, layer=0, table=P, width=5, kv_len=P, q=P, stride=8 * 64, out=P, batch=3, c=2, hq=8, window=0, n_sink=0,
+               scratch=P, nbytes=1 << 40):
+    return l.fc_op_paged_attention(_pool() if pool is None else pool, layer, table, width, kv_len, q, stride, out, batch, c, hq, window, n_sink, scratch,
+                                   nbytes, None)
+
+
+def _reserve(l, pool=None, table=P, width=5, n=3, kv_len=P, refs=P, rows=2, scratch=P, nbytes=1 << 40):
+    return l.fc_op_pages_reserve(_pool() if pool is None else pool, table, width, n, kv_len, refs, rows, None, scratch, nbytes, None)
+
+
+def _compact(l, pool=None, table=P, width=5, n=3, refs=P, scratch=P, nbytes=1 << 40):
+    return l.fc_op_pages_compact(_pool() if pool is None else pool, table, width, n, refs, None, scratch, nbytes, None)
+
+
+def _list(*ids):
+    return (C.c_int32 * max(1, len(ids)))(*ids)
+
+
+def _free(l, seqs=(0, 2), n=None, table=P, width=5, rows=3, kv_len=P, refs=P, pages=10, ps=16, window=0, n_sink=0):
+    a = _list(*seqs) if seqs is not None else None
+    return l.fc_op_pages_free(table, width, rows, kv_len, refs, pages, ps, a, len(seqs) if n is None else n, window, n_sink, None)
+
+
+def _fork(l, src=(0,), dst=(1,), n=None, table=P, width=5, rows=3, kv_len=P, refs=P, pages=10, ps=16):
+    return l.fc_op_pages_fork(table, width, rows, kv_len, refs, pages, ps, _list(*src), _list(*dst), len(dst) if n is None else n, None)
+
+
+BAD_POOLS = [
+    (dict(k=None), lib.FC_ERR_ARG), (dict(v=None), lib.FC_ERR_ARG), (dict(v=P), lib.FC_ERR_ARG), (dict(k=P + 8), lib.FC_ERR_ARG),
+    (dict(dtype=7), lib.FC_ERR_ARG), (dict(n_layers=0), lib.FC_ERR_ARG), (dict(n_pages=0), lib.FC_ERR_ARG), (dict(n_kv_heads=0), lib.FC_ERR_ARG),
+    (dict(page_size=0), lib.FC_ERR_ARG), (dict(head_dim=96), lib.FC_ERR_SHAPE), (dict(slot_stride=60), lib.FC_ERR_ARG),
+    (dict(slot_stride=32), lib.FC_ERR_ARG),                                                  # rows overlap
+    (dict(head_stride=8 * 64), lib.FC_ERR_ARG),                                              # heads overlap
+    (dict(page_stride=0), lib.FC_ERR_ARG), (dict(layer_stride=4 * 16 * 64), lib.FC_ERR_ARG), (dict(page_stride=-4096), lib.FC_ERR_ARG),
+    (dict(head_stride=1 << 46), lib.FC_ERR_ARG), (dict(page_size=1 << 24, n_kv_heads=1), lib.FC_ERR_ARG),
+    (dict(page_size=1 << 26, n_kv_heads=1, head_stride=1 << 32, page_stride=1 << 32, layer_stride=1 << 36), lib.FC_ERR_CAPACITY),
+]
+
+
+@pytest.mark.parametrize("change,code", BAD_POOLS)
+def test_pools_that_are_refused(l, change, code):
+    for call in (_store, _attention, _reserve, _compact):
+        assert call(l, pool=_pool(**change)) == code
+
+
+def test_null_pool(l):
+    none = C.POINTER(lib.fc_pages)()
+    for call in (_store, _attention, _reserve, _compact):
+        assert call(l, pool=none) == lib.FC_ERR_ARG
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(layer=-1), -1), (dict(layer=2), -1), (dict(table=None), -1), (dict(width=0), -1), (dict(kv_len=None), -1), (dict(qkv=None), -1),
+    (dict(qkv=P + 4), -1), (dict(stride=16 * 64 - 4), -1), (dict(stride=16 * 64 + 2), -1), (dict(q=None), -1), (dict(q=P + 8), -1),
+    (dict(batch=0), -1), (dict(c=0), -1), (dict(c=65), -1), (dict(hq=6), -1), (dict(hq=0), -1), (dict(theta=0.0), -1), (dict(theta=float("nan")), -1),
+    (dict(theta=float("inf")), -1), (dict(width=1 << 28), lib.FC_ERR_CAPACITY), (dict(batch=1 << 30, c=4), lib.FC_ERR_CAPACITY)])
+def test_store_refusals(l, kw, code):
+    assert _store(l, **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(layer=-1), -1), (dict(layer=2), -1), (dict(table=None), -1), (dict(width=0), -1), (dict(kv_len=None), -1), (dict(q=None), -1), (dict(q=P + 8), -1),
+    (dict(stride=8 * 64 - 8), -1), (dict(stride=8 * 64 + 4), -1), (dict(out=None), -1), (dict(out=P + 4), -1), (dict(batch=0), -1), (dict(c=0), -1),
+    (dict(c=65), -1), (dict(hq=6), -1), (dict(window=-1), -1), (dict(n_sink=-1), -1), (dict(scratch=None), -1), (dict(scratch=P + 16), -1),
+    (dict(nbytes=0), lib.FC_ERR_CAPACITY), (dict(width=1 << 28), lib.FC_ERR_CAPACITY)])
+def test_attention_refusals(l, kw, code):
+    assert _attention(l, **kw) == code
+
+
+def test_attention_scratch_bytes(l):
+    size = l.fc_op_paged_attention_scratch_bytes
+    good = size(3, 2, 8, 4, 64, lib.FC_BF16)
+    assert good > 0 and good % 256 == 0
+    for bad in ((0, 2, 8, 4, 64, 1), (3, 0, 8, 4, 64, 1), (3, 65, 8, 4, 64, 1), (3, 2, 7, 4, 64, 1), (3, 2, 8, 0, 64, 1), (3, 2, 8, 4, 80, 1), (3, 2, 8, 4, 64, 2)):
+        assert size(*bad) == 0
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(table=None), -1), (dict(width=0), -1), (dict(n=0), -1), (dict(kv_len=None), -1), (dict(refs=None), -1), (dict(rows=0), -1), (dict(rows=65), -1),
+    (dict(scratch=None), -1), (dict(scratch=P + 128), -1), (dict(nbytes=64), lib.FC_ERR_CAPACITY), (dict(width=1 << 28), lib.FC_ERR_CAPACITY)])
+def test_reserve_refusals(l, kw, code):
+    assert _reserve(l, **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(table=None), -1), (dict(width=0), -1), (dict(n=0), -1), (dict(refs=None), -1), (dict(scratch=None), -1), (dict(scratch=P + 128), -1),
+    (dict(nbytes=64), lib.FC_ERR_CAPACITY)])
+def test_compact_refusals(l, kw, code):
+    assert _compact(l, **kw) == code
+
+
+@pytest.mark.parametrize("kw", [
+    dict(seqs=(0, 0)), dict(seqs=(3,)), dict(seqs=(-1,)), dict(n=-1), dict(seqs=None, n=1), dict(table=None), dict(width=0), dict(rows=0), dict(kv_len=None),
+    dict(refs=None), dict(pages=0), dict(ps=0), dict(window=-1), dict(n_sink=-1)])
+def test_free_refusals(l, kw):
+    assert _free(l, **kw) == lib.FC_ERR_ARG
+
+
+@pytest.mark.parametrize("kw", [
+    dict(src=(0, 0), dst=(1, 1)), dict(src=(0,), dst=(0,)), dict(src=(0, 1), dst=(1, 2)), dict(src=(3,)), dict(src=(-1,)), dict(dst=(3,)), dict(dst=(-1,)),
+    dict(n=-1), dict(table=None), dict(width=0), dict(rows=0), dict(kv_len=None), dict(refs=None), dict(pages=0), dict(ps=0)])
+def test_fork_refusals(l, kw):
+    assert _fork(l, **kw) == lib.FC_ERR_ARG
+
+
+def test_nothing_to_free_or_fork(l):
+    assert _free(l, seqs=()) == lib.FC_OK and _fork(l, src=(), dst=()) == lib.FC_OK
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    table, lens, refs = torch.zeros(1, 3, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    q = torch.zeros(1, 2 * 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="CUDA device"):
+        engine.fc_op_paged_attention(q, k, k.clone(), table, lens, 1, 2)
+    with pytest.raises(ValueError, match="same shape and strides"):
+        engine.fc_op_paged_attention(q, k, k.float(), table, lens, 1, 2)
+    with pytest.raises(ValueError, match="same shape and strides"):
+        engine.fc_op_paged_attention(q, k.half(), k.half(), table, lens, 1, 2)
+    with pytest.raises(ValueError, match="same shape and strides"):
+        engine.fc_op_paged_attention(q, k, k.transpose(1, 2).contiguous().transpose(1, 2), table, lens, 1, 2)
+    with pytest.raises(ValueError, match="CUDA device"):
+        engine.fc_op_pages_free(table, lens, refs, 16, [0])
+
+
+# ---- index arithmetic, compiled with the host compiler
+WRAP = """
+#include "fc_paged.h"
+extern "C" {
+int page_of(const int *row, int width, int t, int ps, int n) { return fc::page_of(row, width, t, ps, n); }
+int sees(int p, int t, int w, int s) { return fc::sees(p, t, w, s); }
+int window_first(int p, int w) { return fc::window_first(p, w); }
+int page_unseen(int i, int ps, int len, int w, int s) { return fc::page_unseen(i, ps, len, w, s); }
+int clamp_len(int len, int cap) { return fc::clamp_len(len, cap); }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    d = tmp_path_factory.mktemp("paged")
+    src, so = d / "wrap.cpp", d / "wrap.so"
+    src.write_text(WRAP)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", build.CSRC, "-I", build.INCLUDE, str(src), "-o", str(so)])
+    return C.CDLL(str(so))
+
+
+def test_pages_that_are_not_in_the_pool_have_no_address(host):
+    row = (C.c_int32 * 6)(3, -1, 4, 5, 2 ** 31 - 1, -2 ** 31)
+    got = [host.page_of(row, 6, t, 4, 5) for t in range(0, 32)]
+    assert got == [3] * 4 + [-1] * 4 + [4] * 4 + [-1] * 20
+    assert host.page_of(row, 6, -1, 4, 5) == -1 and host.page_of(row, 6, 2 ** 31 - 1, 1, 5) == -1
+
+
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (1, 0), (1, 3), (4, 0), (4, 2), (7, 100), (2 ** 31 - 1, 5)])
+def test_what_a_row_sees(host, window, n_sink):
+    for p in range(20):
+        want = ref.visible(p, window, n_sink)
+        assert [t for t in range(30) if host.sees(p, t, window, n_sink)] == want
+        assert host.window_first(p, window) == (want[-1] - len([t for t in want if t > p - window]) + 1 if window else 0)
+
+
+def test_pages_released_under_a_window_are_those_that_no_later_row_sees(host):
+    for ps in (1, 3, 4):
+        for window in (1, 2, 5, 9):
+            for n_sink in (0, 1, 4, 7):
+                for n in range(0, 25):
+                    for i in range(9):
+                        seen = any(host.sees(p, t, window, n_sink) for p in range(n, n + 12) for t in range(i * ps, i * ps + ps))
+                        beyond = (i + 1) * ps > n                             # nothing there yet: written later, then seen
+                        assert bool(host.page_unseen(i, ps, n, window, n_sink)) == (not seen and not beyond)
+    assert host.page_unseen(0, 16, 2 ** 31 - 1, 1, 0) and not host.page_unseen(0, 16, -1, 1, 0)
+
+
+def test_lengths_stay_within_the_table(host):
+    assert [host.clamp_len(n, 100) for n in (-2 ** 31, -1, 0, 99, 100, 101, 2 ** 31 - 1)] == [-1, -1, 0, 99, 100, 100, 100]
