@@ -371,5 +371,9 @@ cudaError_t launch_gemm_chain(const UmmaPlan *const *plans, const GemmArgs *args
 
 // Paged K/V cache (k_pages.cu): FC_OK, or why a pool cannot be used.
 int pages_ok(const fc_pages *p);
+// Attention over pages (k_paged_attn.cu).
+struct PagedAttnArgs;
+size_t paged_attn_scratch(int hd, int dtype);
+cudaError_t launch_paged_attn(PagedAttnArgs a, int dtype, int hd, cudaStream_t st);
 
 }  // namespace fc

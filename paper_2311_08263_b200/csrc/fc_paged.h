@@ -17,6 +17,18 @@ struct PageView {
   int n_pages, page_size, n_kv_heads;
 };
 
+struct PagedAttnArgs {
+  PageView pool;
+  const int32_t *table; int width;
+  int cap;                // positions of a table row: width x page_size
+  const int32_t *kv_len;
+  const void *q; long long q_stride;      // elements
+  float *out;             // [batch * c, hq * hd]
+  int batch, c, hq, window, n_sink;       // n_sink is 0 without a window
+  int units;              // kv heads x groups of queries (set by the launcher)
+  float *parts;           // scratch: two parts per worker, [queries][hd] sums and [queries] (max, sum)
+};
+
 // Length of a sequence as the kernels use it: -1 for none, never far beyond the table's `cap` positions (no sum overflows).
 FC_HD int clamp_len(int len, int cap) { return len < 0 ? -1 : len > cap ? cap : len; }
 
@@ -39,5 +51,31 @@ FC_HD int window_first(int p, int window) { return window == 0 || p < window ? 0
 FC_HD bool page_unseen(int i, int page_size, int len, int window, int n_sink) {
   return (long long)(i + 1) * page_size <= (long long)len - window + 1 && (long long)i * page_size >= n_sink;
 }
+
+// The keys that some of the rows at positions len .. len + rows - 1 see, in tiles of `keys` positions: tiles 0 .. sinks - 1, then
+// first .. first + n - sinks - 1.  Rows beyond the table see what is in it (their result is NaN whatever that is).
+struct KeyTiles { int n, sinks, first; };
+FC_HD KeyTiles key_tiles(int len, int rows, int cap, int window, int n_sink, int keys) {
+  KeyTiles t = {0, 0, 0};
+  if (len < 0) return t;
+  const int last = (len + rows < cap ? len + rows : cap) - 1;
+  int low = window_first(len, window);
+  if (low > last) low = last;
+  t.first = low / keys;
+  const int sink_keys = window == 0 ? 0 : n_sink < low ? n_sink : low;
+  t.sinks = sink_keys / keys + (sink_keys % keys != 0);
+  if (t.sinks > t.first) t.sinks = t.first;
+  t.n = t.sinks + last / keys - t.first + 1;
+  return t;
+}
+FC_HD int tile_key(const KeyTiles &t, int i, int keys) { return (i < t.sinks ? i : t.first + i - t.sinks) * keys; }
+
+// All tiles of a call stand in one line: sequence by sequence, unit (kv head, group of queries) by unit, and each of `workers` takes
+// `chunk` of them in a row.  The parts of the unit at [begin, begin + n) and where worker i left its part: place 0 for what a
+// worker begins with, 1 for what it ends with.
+struct UnitParts { int first, last; };
+FC_HD long long chunk_of(long long total, int workers) { return (total + workers - 1) / workers; }
+FC_HD UnitParts unit_parts(long long begin, int n, long long chunk) { return {(int)(begin / chunk), (int)((begin + n - 1) / chunk)}; }
+FC_HD int part_place(long long begin, int worker, long long chunk) { return begin > worker * chunk; }
 
 }  // namespace fc

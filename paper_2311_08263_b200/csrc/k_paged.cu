@@ -1,4 +1,4 @@
-// Paged K/V cache: rotation and K/V write into pages, window attention over pages.
+// Paged K/V cache: rotation and K/V write into pages; entry points of the operations on one layer.
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -66,83 +66,12 @@ __global__ void __launch_bounds__(256) paged_store_kernel(const __grid_constant_
   }
 }
 
-// ------------------------------------------------------------------------------------------------ attention
-struct PagedAttnArgs {
-  PageView pool;
-  const int32_t *table; int width;
-  const int32_t *kv_len;
-  const void *q; long long q_stride;
-  float *out;
-  int c, hq, window, n_sink;
-};
-
-template <typename T> __device__ __forceinline__ float as_float(T v) { return (float)v; }
-
-// One block per row and query head, its warps take turns at the keys, a lane holds HD / 32 elements.
-template <typename T, int HD>
-__global__ void __launch_bounds__(128) paged_attn_kernel(const __grid_constant__ PagedAttnArgs a) {
-  constexpr int E = HD / 32;
-  const int r = blockIdx.x, h = blockIdx.y, b = r / a.c, kvh = h / (a.hq / a.pool.n_kv_heads);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int cap = a.width * a.pool.page_size, len = clamp_len(a.kv_len[b], cap);
-  const int p = len + (r - b * a.c);
-  __shared__ float part[4][HD + 2];
-  float q[E], o[E], m = -INFINITY, l = 0.f;
-  const T *qr = (const T *)a.q + r * a.q_stride + h * HD + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; ++e) { q[e] = as_float(qr[e]) * rsqrtf((float)HD); o[e] = 0.f; }
-  const int32_t *row = a.table + (long long)b * a.width;
-  const int first = len < 0 ? 0 : window_first(p, a.window), sinks = len < 0 ? 0 : min(a.n_sink, first);
-  const int n = len < 0 ? 0 : sinks + p + 1 - first;
-  for (int i = warp; i < n; i += 4) {
-    const int t = i < sinks ? i : first + i - sinks;
-    const int page = page_of(row, a.width, t, a.pool.page_size, a.pool.n_pages);
-    const long long at = (long long)page * a.pool.page_stride + kvh * a.pool.head_stride + (t % a.pool.page_size) * a.pool.slot_stride + lane * E;
-    float s = 0.f, v[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      s = fmaf(q[e], page < 0 ? NAN : as_float(((const T *)a.pool.k)[at + e]), s);
-      v[e] = page < 0 ? NAN : as_float(((const T *)a.pool.v)[at + e]);
-    }
-#pragma unroll
-    for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);
-    const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : expf(m - mn), w = expf(s - mn);
-    l = l * f + w;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * f + w * v[e];
-    m = mn;
-  }
-#pragma unroll
-  for (int e = 0; e < E; ++e) part[warp][lane * E + e] = o[e];
-  if (lane == 0) { part[warp][HD] = m; part[warp][HD + 1] = l; }
-  __syncthreads();
-  for (int e = threadIdx.x; e < HD; e += 128) {
-    float M = -INFINITY, den = 0.f, sum = 0.f;
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, part[w][HD]);
-    for (int w = 0; w < 4; ++w) {
-      const float f = part[w][HD] == -INFINITY && part[w][HD + 1] == 0.f ? 0.f : expf(part[w][HD] - M);
-      den += f * part[w][HD + 1];
-      sum += f * part[w][e];
-    }
-    a.out[((long long)r * a.hq + h) * HD + e] = den == 0.f ? 0.f : sum / den;
-  }
-}
-
-template <typename T>
-cudaError_t launch_paged_attn(const PagedAttnArgs &a, int hd, int batch, cudaStream_t st) {
-  const dim3 grid(batch * a.c, a.hq);
-  if (hd == 128) paged_attn_kernel<T, 128><<<grid, 128, 0, st>>>(a);
-  else if (hd == 64) paged_attn_kernel<T, 64><<<grid, 128, 0, st>>>(a);
-  else paged_attn_kernel<T, 32><<<grid, 128, 0, st>>>(a);
-  return cudaGetLastError();
-}
-
 // ------------------------------------------------------------------------------------------------ arguments
 int call_ok(const fc_pages *pages, int layer, const int32_t *table, int width, const int32_t *kv_len, int batch, int c, int hq) {
   if (int rc = pages_ok(pages)) return rc;
   if (!table || !kv_len || layer < 0 || layer >= pages->n_layers || width < 1 || batch < 1 || c < 1 || c > 64 || hq < 1) return FC_ERR_ARG;
   if (hq % pages->n_kv_heads) return FC_ERR_ARG;
-  if ((long long)width * pages->page_size > INT_MAX - 1024 || (long long)batch * c > INT_MAX / 2 || hq > 65535) return FC_ERR_CAPACITY;
+  if ((long long)width * pages->page_size > INT_MAX - 1024 || (long long)batch * c * hq > INT_MAX / 2 || hq > 65535) return FC_ERR_CAPACITY;
   return FC_OK;
 }
 
@@ -185,7 +114,7 @@ extern "C" size_t fc_op_paged_attention_scratch_bytes(int32_t batch, int32_t c, 
                                                       int32_t dtype) {
   if (batch < 1 || c < 1 || c > 64 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return 0;
   if ((head_dim != 32 && head_dim != 64 && head_dim != 128) || (dtype != FC_F32 && dtype != FC_BF16)) return 0;
-  return 256;
+  return (paged_attn_scratch(head_dim, dtype) + 255) / 256 * 256;
 }
 
 extern "C" int fc_op_paged_attention(const fc_pages *pages, int32_t layer, const int32_t *table, int32_t table_width, const int32_t *kv_len,
@@ -196,11 +125,9 @@ extern "C" int fc_op_paged_attention(const fc_pages *pages, int32_t layer, const
   if (!q || !out || !scratch || ((uintptr_t)q | (uintptr_t)out) % 16 || (uintptr_t)scratch % 256 || q_stride % per ||
       q_stride < (int64_t)n_heads * hd || window < 0 || n_sink < 0) return FC_ERR_ARG;
   if (scratch_bytes < fc_op_paged_attention_scratch_bytes(batch, c, n_heads, pages->n_kv_heads, hd, pages->dtype)) return FC_ERR_CAPACITY;
-  PagedAttnArgs a;
+  PagedAttnArgs a; memset(&a, 0, sizeof a);
   a.pool = view_of(pages, layer);
-  a.table = table; a.width = table_width; a.kv_len = kv_len; a.q = q; a.q_stride = q_stride; a.out = out;
-  a.c = c; a.hq = n_heads; a.window = window; a.n_sink = n_sink;
-  const cudaError_t e = pages->dtype == FC_F32 ? launch_paged_attn<float>(a, hd, batch, (cudaStream_t)cuda_stream)
-                                               : launch_paged_attn<__nv_bfloat16>(a, hd, batch, (cudaStream_t)cuda_stream);
-  return e == cudaSuccess ? FC_OK : FC_ERR_CUDA;
+  a.table = table; a.width = table_width; a.cap = table_width * pages->page_size; a.kv_len = kv_len; a.q = q; a.q_stride = q_stride; a.out = out;
+  a.batch = batch; a.c = c; a.hq = n_heads; a.window = window; a.n_sink = window > 0 ? n_sink : 0; a.parts = (float *)scratch;
+  return launch_paged_attn(a, pages->dtype, hd, (cudaStream_t)cuda_stream) == cudaSuccess ? FC_OK : FC_ERR_CUDA;
 }
