@@ -374,6 +374,6 @@ int pages_ok(const fc_pages *p);
 // Attention over pages (k_paged_attn.cu).
 struct PagedAttnArgs;
 size_t paged_attn_scratch(int hd, int dtype);
-cudaError_t launch_paged_attn(PagedAttnArgs a, int dtype, int hd, cudaStream_t st);
+cudaError_t launch_paged_attn(const PagedAttnArgs &a, int dtype, int hd, cudaStream_t st);
 
 }  // namespace fc

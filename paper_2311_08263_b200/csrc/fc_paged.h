@@ -25,7 +25,7 @@ struct PagedAttnArgs {
   const void *q; long long q_stride;      // elements
   float *out;             // [batch * c, hq * hd]
   int batch, c, hq, window, n_sink;       // n_sink is 0 without a window
-  int units;              // kv heads x groups of queries (set by the launcher)
+  int groups;             // groups of queries of a kv head (set by the launcher)
   float *parts;           // scratch: two parts per worker, [queries][hd] sums and [queries] (max, sum)
 };
 
@@ -77,5 +77,15 @@ struct UnitParts { int first, last; };
 FC_HD long long chunk_of(long long total, int workers) { return (total + workers - 1) / workers; }
 FC_HD UnitParts unit_parts(long long begin, int n, long long chunk) { return {(int)(begin / chunk), (int)((begin + n - 1) / chunk)}; }
 FC_HD int part_place(long long begin, int worker, long long chunk) { return begin > worker * chunk; }
+
+// CTAs of a cluster per unit where one launch of clusters does the work of the line and the kernel that joins its parts, 0 otherwise.  All
+// clusters have to run at once, and no warp may have more than a few tiles, whatever the lengths are (only the table's bound on them is known).
+inline int paged_cluster(int batch, int units, int cap, int c, int window, int n_sink, int keys, int warps, int sms) {
+  const long long most = window > 0 && (long long)window + c + n_sink < cap ? (long long)window + c + n_sink + 2 * keys : cap;
+  const long long tiles = (most + keys - 1) / keys;
+  int ctas = 1;
+  while (ctas < 8 && tiles > ctas * warps && (long long)batch * units * ctas * 2 <= sms - 20) ctas *= 2;
+  return (long long)batch * units * ctas <= sms && tiles <= 4ll * warps * ctas ? ctas : 0;
+}
 
 }  // namespace fc

@@ -1,13 +1,16 @@
 // Window attention over pages: out = softmax(q.k / sqrt(hd)) v over the keys that a row sees, keys and values behind a table of pages.
 //
-// paged_mma_kernel (bf16).  One CTA per SM.  The work is a line of key tiles (32 keys), sequence by sequence and unit by unit (a kv head
-// and 16 queries: window rows x heads of the group), cut into equal pieces, one per CTA, whatever the lengths of the sequences: the
-// launch depends on no length, and a batch of ragged caches is as balanced as one long cache.  The warps of a CTA take turns at its tiles.
-// A warp loads its own tiles into its own ring (cp.async, 16 bytes a lane, the lanes look up the pages of the tile's keys), so that it waits for nobody while
-// it streams, and the ring runs on across units.  Scores, probabilities and the 16 x hd output stay in its registers; the
-// accumulators of Q.K^T are the A operand of P.V as they are.  Where a unit ends (or the CTA's piece), the warps exchange their results through
-// shared memory, each adds up a part of the columns, and the unit is written; a unit that several CTAs share goes to scratch as un-normalised parts.
-// paged_combine_kernel adds those up in order, and writes the rows that see nothing.
+// paged_mma_kernel (bf16).  A unit is a kv head of a sequence and 8 or 16 queries (window rows x heads of the group); its keys come in tiles of
+// 16.  The products are taken with the keys as rows, S^T = K.Q^T and O^T = V^T.P^T, so that the 16 rows of an MMA are keys and
+// head elements, always full, and only its 8 columns are queries.  The warps of a CTA take turns at the tiles of its piece of work.  A warp loads its
+// own tiles into its own ring (cp.async, 16 bytes a lane; the lanes look up the pages of the tile's keys), so that it waits for nobody while it
+// streams.  Scores, probabilities and the output stay in its registers.  Where a unit (or the CTA's piece of it) ends, the warps
+// exchange their sums through shared memory and each adds up a part of the elements.
+//   Line: one CTA per SM.  The tiles of all units stand in one line, sequence by sequence, cut into equal pieces, one per CTA, whatever
+// the lengths: the launch depends on none, a batch of ragged caches is as balanced as one long cache, and the rings run on from unit to unit.  A
+// unit that several CTAs share goes to scratch as un-normalised sums, which paged_combine_kernel adds up in order.
+//   Cluster: for tables that hold little, a cluster per unit, whose CTAs take equal shares of its tiles and join them through distributed
+// shared memory: one launch, no scratch.
 //
 // Probabilities enter the tensor cores as three bf16 parts (their sum has all 24 bits), a tile's product is added to the output in fp32: what is rounded
 // is what is stored in the cache, nothing else.  (Two parts leave 1.5e-6, relative, of the result.)
@@ -22,21 +25,22 @@ namespace fc {
 
 namespace {
 
-constexpr int kKeys = 32;              // keys per tile
+constexpr int kKeys = 16;              // keys per tile
+constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kWorkers = 148;          // CTAs on the line: one per SM
 
 template <int HD>
 struct PagedCfg {
-  static constexpr int W = HD == 64 ? 8 : 4;                       // warps
-  static constexpr int S = HD == 32 ? 8 : 3;                       // stages of a warp's ring
   static constexpr uint32_t kHalf = kKeys * HD * 2, kTile = 2 * kHalf;
-  static constexpr int NB = HD / 8, OWN = NB / W;                  // column blocks of the output; of them a warp's own in the exchange
-  static constexpr size_t kRing = (size_t)W * S * kTile;
-  static constexpr size_t kExchange = (size_t)W * (W - 1) * OWN * 32 * 16;
+  static constexpr int S = HD == 128 ? 3 : 6;                      // stages of a warp's ring
+  static constexpr int DB = HD / 16;                               // blocks of 16 elements of the output
+  static constexpr uint32_t kRing = kWarps * S * kTile;
+  static constexpr uint32_t kExchange = DB * (kWarps - 1) * 512;   // a block of 8 queries at a time
   static constexpr size_t kSmem = 128 + kRing + kExchange;
 };
 
-// Byte offset of 16-byte piece `ch` of key `r` in a tile: rows of 128 bytes (two side by side in sub-tiles at hd 128), pieces
-// permuted so that eight rows at one piece lie in different banks.
+// Byte offset of 16-byte piece `ch` of key `r` in a tile: rows of 128 bytes (hd 128: two sub-tiles), pieces permuted so that eight
+// rows at one piece lie in different banks.
 template <int HD>
 __device__ __forceinline__ uint32_t poff(int r, int ch) {
   if (HD == 32) return (uint32_t)r * 64u + (uint32_t)((ch ^ ((r >> 1) & 3)) << 4);
@@ -45,40 +49,54 @@ __device__ __forceinline__ uint32_t poff(int r, int ch) {
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+// 8 x 8 transpose of 16-bit elements across a warp
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+// What a part with maximum m and sum l counts against a maximum M; one that saw nothing counts nothing.
+__device__ __forceinline__ float part_weight(float2 part, float M, float sl2) {
+  return part.x == -INFINITY && part.y == 0.f ? 0.f : ex2((part.x - M) * sl2);
+}
+__device__ __forceinline__ float quiet_nan() { return __int_as_float(0x7fffffff); }
 
-// Units of a sequence, tiles of a unit, of sequence b.
 __device__ __forceinline__ KeyTiles seq_tiles(const PagedAttnArgs &a, int b, int &len) {
   len = clamp_len(a.kv_len[b], a.cap);
   return key_tiles(len, a.c, a.cap, a.window, a.n_sink, kKeys);
 }
 
-// A place on the line of tiles: tile t of unit u of sequence b.
+// A place on the line of tiles: tile t of a unit (kv head, group of queries) of sequence b.
 struct Place {
-  int b, u, t, len;
+  int b, kvh, qg, t, len;
   KeyTiles k;
 };
-// The next place `step` tiles on; the caller knows that there is one.
-__device__ __forceinline__ void move_on(const PagedAttnArgs &a, Place &p, int step) {
+// `step` tiles on; false behind the last one.  *unit: whether another unit is reached.
+__device__ __forceinline__ void move_on(const PagedAttnArgs &a, Place &p, int step, bool &unit) {
   p.t += step;
+  unit = p.t >= p.k.n;
   while (p.t >= p.k.n) {
     p.t -= p.k.n;
-    if (++p.u == a.units) {
-      p.u = 0;
-      do {
-        if (++p.b >= a.batch) { p.k.n = 0x7fffffff; return; }
-        p.k = seq_tiles(a, p.b, p.len);
-      } while (p.k.n == 0);
+    if (++p.qg == a.groups) {
+      p.qg = 0;
+      if (++p.kvh == a.pool.n_kv_heads) {
+        p.kvh = 0;
+        do {
+          if (++p.b >= a.batch) { p.k.n = 0x7fffffff; return; }
+          p.k = seq_tiles(a, p.b, p.len);
+        } while (p.k.n == 0);
+      }
     }
   }
 }
 
 // Tiles of the whole call, and of the sequences in front of sequence `upto` (a warp does this together).
 __device__ __forceinline__ void count_tiles(const PagedAttnArgs &a, int upto, long long &total, long long &before) {
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, units = a.groups * a.pool.n_kv_heads;
   long long all = 0, some = 0;
   for (int b = lane; b < a.batch; b += 32) {
     int len;
-    const long long n = (long long)seq_tiles(a, b, len).n * a.units;
+    const long long n = (long long)seq_tiles(a, b, len).n * units;
     all += n;
     if (b < upto) some += n;
   }
@@ -92,14 +110,14 @@ __device__ __forceinline__ void count_tiles(const PagedAttnArgs &a, int upto, lo
 }
 // The place of tile f of the line (a warp together; f is inside the line).
 __device__ __forceinline__ Place find_place(const PagedAttnArgs &a, long long f) {
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, units = a.groups * a.pool.n_kv_heads;
   long long base = 0;
-  Place p = {0, 0, 0, -1, {0, 0, 0}};
+  Place p = {0, 0, 0, 0, -1, {0, 0, 0}};
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
     int len = -1;
     KeyTiles k = {0, 0, 0};
     if (b0 + lane < a.batch) k = seq_tiles(a, b0 + lane, len);
-    long long x = (long long)k.n * a.units;
+    long long x = (long long)k.n * units;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(0xffffffffu, x, o);
@@ -113,9 +131,11 @@ __device__ __forceinline__ Place find_place(const PagedAttnArgs &a, long long f)
       p.k.first = __shfl_sync(0xffffffffu, k.first, w);
       p.len = __shfl_sync(0xffffffffu, len, w);
       p.b = b0 + w;
-      const long long at = f - (base + __shfl_sync(0xffffffffu, x, w) - (long long)p.k.n * a.units);
-      p.u = (int)(at / p.k.n);
-      p.t = (int)(at - (long long)p.u * p.k.n);
+      const long long at = f - (base + __shfl_sync(0xffffffffu, x, w) - (long long)p.k.n * units);
+      const int u = (int)(at / p.k.n);
+      p.t = (int)(at - (long long)u * p.k.n);
+      p.kvh = u / a.groups;
+      p.qg = u - p.kvh * a.groups;
       return p;
     }
     base += __shfl_sync(0xffffffffu, x, 31);
@@ -125,77 +145,102 @@ __device__ __forceinline__ Place find_place(const PagedAttnArgs &a, long long f)
 
 // Result of a query: un-normalised sums over `den`.  A row that sees nothing is 0, one beyond the table NaN.
 __device__ __forceinline__ float result_scale(const PagedAttnArgs &a, int pos, float den) {
-  return pos >= a.cap ? __int_as_float(0x7fffffff) : den == 0.f ? 0.f : 1.0f / den;
+  return pos >= a.cap ? quiet_nan() : den == 0.f ? 0.f : 1.0f / den;
 }
 
-template <int HD>
-__global__ void __launch_bounds__(PagedCfg<HD>::W * 32, 1) paged_mma_kernel(const __grid_constant__ PagedAttnArgs a) {
+// QN: blocks of 8 queries of a unit.  LINE: the line of tiles, else a cluster per unit (grid: CTAs of the cluster, units, sequences).
+template <int HD, int QN, bool LINE>
+__global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_constant__ PagedAttnArgs a) {
   using C = PagedCfg<HD>;
-  constexpr int W = C::W, S = C::S, KS = HD / 16, NT = kKeys / 8, NB = C::NB, OWN = C::OWN;
+  constexpr int W = kWarps, S = C::S, KS = HD / 16, DB = C::DB, Q = 8 * QN;
   constexpr int PER = HD / 8, RPI = 32 / PER;            // 16-byte pieces of a row; rows that the lanes of a warp load at once
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  constexpr int OWN = (DB + W - 1) / W;                  // blocks of elements that a warp adds up
+  if (LINE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
-  __shared__ float2 ml[W][16];                           // (max, sum) per warp and query
+  __shared__ float2 ml[W][Q];                            // (max, sum) per warp and query
   __shared__ unsigned int bad_keys[W][S];                // keys of a tile whose page is missing
+  __shared__ float2 ml_cta[Q];
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, t4 = lane & 3;
   const uint32_t base = (smem_u32(smem_raw) + 127u) & ~127u;
+  unsigned char *base_g = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t ring = base + (uint32_t)warp * (S * C::kTile);
-  unsigned char *ring_g = smem_raw + (ring - smem_u32(smem_raw));
-  float4 *exchange = reinterpret_cast<float4 *>(smem_raw + (base - smem_u32(smem_raw)) + C::kRing);
+  float4 *exchange = reinterpret_cast<float4 *>(base_g + C::kRing);
 
-  long long total, unused;
-  count_tiles(a, 0, total, unused);
-  const long long chunk = chunk_of(total, gridDim.x), f0 = chunk * blockIdx.x;
-  if (f0 >= total) return;
-  const int n_mine = (int)(total - f0 < chunk ? total - f0 : chunk);
-  Place seg = find_place(a, f0);                         // where the segment (a unit's tiles in this piece) begins
-  Place ld = seg;                                        // the tile that is requested next
-  if (warp < n_mine && warp > 0) move_on(a, ld, warp);
-  int ld_i = warp;
-  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c, nqg = a.units / a.pool.n_kv_heads;
+  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
+  Place seg;                                             // where the segment (a unit's tiles in this CTA's piece) begins
+  int n_mine;
+  if (LINE) {
+    long long total, unused;
+    count_tiles(a, 0, total, unused);
+    const long long chunk = chunk_of(total, gridDim.x), f0 = chunk * blockIdx.x;
+    if (f0 >= total) return;
+    n_mine = (int)(total - f0 < chunk ? total - f0 : chunk);
+    seg = find_place(a, f0);
+  } else {
+    seg.b = blockIdx.z; seg.kvh = blockIdx.y / a.groups; seg.qg = blockIdx.y - seg.kvh * a.groups;
+    seg.k = seq_tiles(a, seg.b, seg.len);
+    const int cut = (seg.k.n + gridDim.x - 1) / gridDim.x;
+    seg.t = cut * blockIdx.x;
+    n_mine = max(0, min(cut, seg.k.n - seg.t));
+  }
 
-  // the lanes' keys of the next tile: page and offset are looked up a tile ahead of the copies
-  int next_key = 0, next_page = -1;
-  bool next_seen = false;
+  // ---- what is requested next: a tile of 16 keys, the lanes' keys (twice) looked up a tile ahead of the copies
+  Place ld = seg;
+  int ld_i = warp, see_from = 0, see_to = -1;            // keys that some query of the unit sees: the sinks, and from .. to
+  long long next_off = -1;
+  unsigned int next_bad = 0;
+  auto unit_keys = [&]() {
+    see_from = window_first(ld.len + ld.qg * Q / group, a.window);                       // the first row's window reaches furthest back
+    see_to = min(ld.len + min(nq - 1, ld.qg * Q + Q - 1) / group, a.cap - 1);
+  };
   auto look_up = [&]() {
-    next_seen = false;
-    if (ld_i < n_mine) {
-      const int qg = ld.u % nqg;
-      const int p_first = ld.len + qg * 16 / group, p_last = ld.len + min(nq - 1, qg * 16 + 15) / group;
-      next_key = tile_key(ld.k, ld.t, kKeys) + lane;
-      // keys that some row of the unit sees: the first row's window reaches furthest back
-      next_seen = next_key <= p_last && (next_key >= window_first(p_first, a.window) || next_key < a.n_sink) && next_key < a.cap;
-      if (next_seen) next_page = page_of(a.table + (long long)ld.b * a.width, a.width, next_key, a.pool.page_size, a.pool.n_pages);
+    const int t = tile_key(ld.k, ld.t, kKeys) + (lane & 15);
+    next_off = -1;
+    bool bad = false;
+    if (t <= see_to && (t >= see_from || t < a.n_sink)) {
+      const int i = t / a.pool.page_size, page = a.table[(long long)ld.b * a.width + i];
+      bad = page < 0 || page >= a.pool.n_pages;
+      if (!bad) next_off = (long long)page * a.pool.page_stride + (long long)(t - i * a.pool.page_size) * a.pool.slot_stride;
     }
+    next_bad = __ballot_sync(0xffffffffu, bad) & 0xffffu;
   };
   auto request = [&](int stage) {
     if (ld_i < n_mine) {
-      const int kvh = ld.u / nqg;
-      long long off = -1;
-      if (next_seen && next_page >= 0)
-        off = (long long)next_page * a.pool.page_stride + (long long)(next_key % a.pool.page_size) * a.pool.slot_stride;
-      const unsigned int bad = __ballot_sync(0xffffffffu, next_seen && next_page < 0);
-      if (lane == 0) bad_keys[warp][stage] = bad;
+      if (lane == 0) bad_keys[warp][stage] = next_bad;
       const uint32_t kb = ring + stage * C::kTile;
-      const __nv_bfloat16 *k0 = (const __nv_bfloat16 *)a.pool.k + kvh * a.pool.head_stride + (lane % PER) * 8;
-      const __nv_bfloat16 *v0 = (const __nv_bfloat16 *)a.pool.v + kvh * a.pool.head_stride + (lane % PER) * 8;
+      const __nv_bfloat16 *k0 = (const __nv_bfloat16 *)a.pool.k + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
+      const __nv_bfloat16 *v0 = (const __nv_bfloat16 *)a.pool.v + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
 #pragma unroll
       for (int i = 0; i < kKeys / RPI; ++i) {
         const int r = i * RPI + lane / PER;
-        const long long o = __shfl_sync(0xffffffffu, off, r);
+        const long long o = __shfl_sync(0xffffffffu, next_off, r);
         const uint32_t d = kb + poff<HD>(r, lane % PER), bytes = o < 0 ? 0u : 16u;      // keys that no row sees become zeros
         copy16(d, k0 + (o < 0 ? 0 : o), bytes);
         copy16(d + C::kHalf, v0 + (o < 0 ? 0 : o), bytes);
       }
       ld_i += W;
-      if (ld_i < n_mine) move_on(a, ld, W);
-      look_up();
+      if (ld_i < n_mine) {
+        if (LINE) {
+          bool unit;
+          move_on(a, ld, W, unit);
+          if (unit) unit_keys();
+        } else {
+          ld.t += W;
+        }
+        look_up();
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  look_up();
+  if (ld_i < n_mine) {
+    bool unit;
+    if (!LINE) ld.t += warp;
+    else if (warp) move_on(a, ld, warp, unit);
+    unit_keys();
+    look_up();
+  }
 #pragma unroll
   for (int s = 0; s < S - 1; ++s) request(s);
 
@@ -205,29 +250,37 @@ __global__ void __launch_bounds__(PagedCfg<HD>::W * 32, 1) paged_mma_kernel(cons
   while (true) {
     // ---- a segment: tiles done .. done + seg_n of the piece, tiles seg.t .. of the unit
     const int seg_n = min(n_mine - done, seg.k.n - seg.t);
-    const int kvh = seg.u / nqg, qg = seg.u - kvh * nqg;
-    const int q0 = qg * 16, q_last = min(nq - 1, q0 + 15);
-    int pos[2], low[2];
-    uint32_t qf[KS][4];
+    const int q0 = seg.qg * Q, q_last = min(nq - 1, q0 + Q - 1);
+    // a lane's queries as columns of the scores: 2 t4 and 2 t4 + 1 of each block; as columns of Q^T: g4
+    int pos[QN][2], low[QN][2];
+    uint32_t qf[QN][KS][2];
 #pragma unroll
-    for (int hh = 0; hh < 2; ++hh) {
-      const int q = min(q0 + g4 + hh * 8, nq - 1), j = q / group, h = kvh * group + q - j * group;
-      pos[hh] = seg.len + j;
-      low[hh] = window_first(pos[hh], a.window);
+    for (int n = 0; n < QN; ++n) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        pos[n][x] = seg.len + min(q0 + n * 8 + t4 * 2 + x, nq - 1) / group;
+        low[n][x] = window_first(pos[n][x], a.window);
+      }
+      const int q = min(q0 + n * 8 + g4, nq - 1), j = q / group, h = seg.kvh * group + q - j * group;
       const __nv_bfloat16 *qr = (const __nv_bfloat16 *)a.q + ((long long)seg.b * a.c + j) * a.q_stride + h * HD + t4 * 2;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        qf[ks][hh] = *reinterpret_cast<const uint32_t *>(qr + ks * 16);
-        qf[ks][hh + 2] = *reinterpret_cast<const uint32_t *>(qr + ks * 16 + 8);
+        qf[n][ks][0] = *reinterpret_cast<const uint32_t *>(qr + ks * 16);
+        qf[n][ks][1] = *reinterpret_cast<const uint32_t *>(qr + ks * 16 + 8);
       }
     }
     const int p_first = seg.len + q0 / group, p_last = seg.len + q_last / group;
-    const int low_first = window_first(p_first, a.window), low_last = window_first(p_last, a.window);
-    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f}, o[NB][4];
+    const int low_last = window_first(p_last, a.window);
+    float m_run[QN][2], l_run[QN][2], o[QN][DB][4];
 #pragma unroll
-    for (int n = 0; n < NB; ++n)
+    for (int n = 0; n < QN; ++n) {
+      m_run[n][0] = m_run[n][1] = -INFINITY;
+      l_run[n][0] = l_run[n][1] = 0.f;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[n][d][x] = 0.f;
+    }
 
     for (; i < done + seg_n; i += W) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
@@ -236,227 +289,263 @@ __global__ void __launch_bounds__(PagedCfg<HD>::W * 32, 1) paged_mma_kernel(cons
       const int key0 = tile_key(seg.k, seg.t + i - done, kKeys);
       const uint32_t kb = ring + stage * C::kTile, vb = kb + C::kHalf;
       const unsigned int bad = bad_keys[warp][stage];
-      // ---- S = Q.K^T: 16 queries x 32 keys
-      float s[NT][4];
+      // ---- S^T = K.Q^T: 16 keys x 8 QN queries; the k range in two halves (shorter chains of MMAs)
+      float s[QN][4], s2[QN][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < QN; ++n)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) s[n][x] = 0.f;
+        for (int x = 0; x < 4; ++x) s[n][x] = s2[n][x] = 0.f;
 #pragma unroll
-      for (int k2 = 0; k2 < KS / 2; ++k2) {
-        uint32_t kf[NT][4];
+      for (int ks = 0; ks < KS; ks += 2) {
+        uint32_t k0[4], k1[4];
+        ldsm4(kb + poff<HD>(lane & 15, ks * 2 + (lane >> 4)), k0);
+        ldsm4(kb + poff<HD>(lane & 15, ks * 2 + 2 + (lane >> 4)), k1);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) ldsm4(kb + poff<HD>(n * 8 + (lane & 7), k2 * 4 + (lane >> 3)), kf[n]);
+        for (int n = 0; n < QN; ++n) mma16816(s[n], k0, qf[n][ks][0], qf[n][ks][1]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) mma16816(s[n], qf[2 * k2], kf[n][0], kf[n][1]);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma16816(s[n], qf[2 * k2 + 1], kf[n][2], kf[n][3]);
+        for (int n = 0; n < QN; ++n) mma16816(s2[n], k1, qf[n][ks + 1][0], qf[n][ks + 1][1]);
       }
+#pragma unroll
+      for (int n = 0; n < QN; ++n)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[n][x] += s2[n][x];
       // ---- what the rows do not see, and keys without a page
       const bool masked = key0 + kKeys - 1 > p_first || (key0 < low_last && key0 + kKeys > a.n_sink);
       if (masked || bad) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < QN; ++n)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const int kk = n * 8 + t4 * 2 + (x & 1), t = key0 + kk;
-            if (bad >> kk & 1u) s[n][x] = __int_as_float(0x7fffffff);
-            if (t > pos[x >> 1] || (t < low[x >> 1] && t >= a.n_sink)) s[n][x] = -INFINITY;
+            const int kk = g4 + (x >> 1) * 8, t = key0 + kk;
+            if (bad >> kk & 1u) s[n][x] = quiet_nan();
+            if (t > pos[n][x & 1] || (t < low[n][x & 1] && t >= a.n_sink)) s[n][x] = -INFINITY;
           }
       }
-      // ---- running maximum
-      float mx[2] = {m_run[0], m_run[1]}, corr[2];
+      // ---- running maximum of the lane's queries
+      float corr[QN][2];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        mx[0] = fmaxf(mx[0], fmaxf(s[n][0], s[n][1]));
-        mx[1] = fmaxf(mx[1], fmaxf(s[n][2], s[n][3]));
-      }
+      for (int n = 0; n < QN; ++n)
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        mx[hh] = fmaxf(mx[hh], __shfl_xor_sync(0xffffffffu, mx[hh], 1));
-        mx[hh] = fmaxf(mx[hh], __shfl_xor_sync(0xffffffffu, mx[hh], 2));
-        corr[hh] = mx[hh] == m_run[hh] ? 1.f : ex2((m_run[hh] - mx[hh]) * sl2);           // first tile: 2^-inf = 0
-        m_run[hh] = mx[hh];
-        l_run[hh] *= corr[hh];
-      }
-      // ---- probabilities
-      const float mb[2] = {mx[0] == -INFINITY ? 0.f : mx[0] * sl2, mx[1] == -INFINITY ? 0.f : mx[1] * sl2};
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[n][x] = ex2(fmaf(s[n][x], sl2, -mb[x >> 1]));
-        l_run[0] += s[n][0] + s[n][1];
-        l_run[1] += s[n][2] + s[n][3];
-      }
+        for (int x = 0; x < 2; ++x) {
+          float mx = fmaxf(m_run[n][x], fmaxf(s[n][x], s[n][x + 2]));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          corr[n][x] = mx == m_run[n][x] ? 1.f : ex2((m_run[n][x] - mx) * sl2);           // first tile: 2^-inf = 0
+          m_run[n][x] = mx;
+          const float mb = mx == -INFINITY ? 0.f : mx * sl2;
+          s[n][x] = ex2(fmaf(s[n][x], sl2, -mb));
+          s[n][x + 2] = ex2(fmaf(s[n][x + 2], sl2, -mb));
+          l_run[n][x] = fmaf(l_run[n][x], corr[n][x], s[n][x] + s[n][x + 2]);
+        }
       // ---- values that are not finite, in a tile that some rows see more of than others: a probability of zero would
       // still carry them to the rows that do not see them.  Those keys are added row by row and taken out of the tile.
       if (masked && p_first != p_last) {
+        unsigned char *vg = base_g + (vb - base);
         unsigned int odd = 0;
         for (int e = lane; e < kKeys * PER; e += 32) {
-          const int r = e / PER;
-          const uint4 x = *reinterpret_cast<const uint4 *>(ring_g + (vb - ring) + poff<HD>(r, e % PER));
+          const uint4 x = *reinterpret_cast<const uint4 *>(vg + poff<HD>(e / PER, e % PER));
           const uint32_t y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if ((y[c] & 0x7f80u) == 0x7f80u || (y[c] & 0x7f800000u) == 0x7f800000u) odd |= 1u << r;
+          for (int w = 0; w < 4; ++w)
+            if ((y[w] & 0x7f80u) == 0x7f80u || (y[w] & 0x7f800000u) == 0x7f800000u) odd |= 1u << (e / PER);
         }
         odd = __reduce_or_sync(0xffffffffu, odd);
         if (odd) {
 #pragma unroll
-          for (int n = 0; n < NB; ++n) { o[n][0] *= corr[0]; o[n][1] *= corr[0]; o[n][2] *= corr[1]; o[n][3] *= corr[1]; }
-          corr[0] = corr[1] = 1.f;
+          for (int n = 0; n < QN; ++n) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) o[n][d][x] *= corr[n][x & 1];
+            corr[n][0] = corr[n][1] = 1.f;
+          }
           for (unsigned int left = odd; left; left &= left - 1) {
-            const int kk = __ffs(left) - 1, t = key0 + kk;
-            float p[2] = {0.f, 0.f};
+            const int kk = __ffs(left) - 1;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < QN; ++n)
 #pragma unroll
-              for (int x = 0; x < 4; ++x)
-                if (n == kk >> 3 && (x & 1) == (kk & 1)) p[x >> 1] = s[n][x];
+              for (int x = 0; x < 2; ++x) {
+                const float p = __shfl_sync(0xffffffffu, kk < 8 ? s[n][x] : s[n][x + 2], (kk & 7) * 4 + t4);
+                if (!sees(pos[n][x], key0 + kk, a.window, a.n_sink)) continue;
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-              p[hh] = __shfl_sync(0xffffffffu, p[hh], (lane & ~3) | ((kk & 7) >> 1));
-              if (!sees(pos[hh], t, a.window, a.n_sink)) continue;
+                for (int d = 0; d < DB; ++d)
 #pragma unroll
-              for (int n = 0; n < NB; ++n) {
-                const uint32_t y = *reinterpret_cast<const uint32_t *>(ring_g + (vb - ring) + poff<HD>(kk, n) + t4 * 4);
-                o[n][2 * hh] = fmaf(p[hh], low_half(y), o[n][2 * hh]);
-                o[n][2 * hh + 1] = fmaf(p[hh], high_half(y), o[n][2 * hh + 1]);
+                  for (int e = 0; e < 2; ++e) {
+                    const __nv_bfloat16 y = *reinterpret_cast<const __nv_bfloat16 *>(vg + poff<HD>(kk, d * 2 + e) + g4 * 2);
+                    o[n][d][2 * e + x] = fmaf(p, __bfloat162float(y), o[n][d][2 * e + x]);
+                  }
               }
-            }
           }
           __syncwarp();
           for (int e = lane; e < kKeys * PER; e += 32)
-            if (odd >> (e / PER) & 1u) *reinterpret_cast<uint4 *>(ring_g + (vb - ring) + poff<HD>(e / PER, e % PER)) = make_uint4(0, 0, 0, 0);
+            if (odd >> (e / PER) & 1u) *reinterpret_cast<uint4 *>(vg + poff<HD>(e / PER, e % PER)) = make_uint4(0, 0, 0, 0);
           __syncwarp();
         }
       }
-      // ---- O = corr O + P.V, the score registers as the A operand
-      uint32_t pf[NT / 2][3][4];
+      // ---- O^T = corr O^T + V^T.P^T; the scores' registers, transposed in 8 x 8 blocks, are the B operand
+      uint32_t pf[QN][3][2];
 #pragma unroll
-      for (int kk = 0; kk < NT / 2; ++kk)
+      for (int n = 0; n < QN; ++n)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          float p0 = s[2 * kk + (x >> 1)][(x & 1) * 2], p1 = s[2 * kk + (x >> 1)][(x & 1) * 2 + 1];
+        for (int x = 0; x < 2; ++x) {
+          float p0 = s[n][2 * x], p1 = s[n][2 * x + 1];
 #pragma unroll
           for (int part = 0; part < 3; ++part) {
-            pf[kk][part][x] = pack2(p0, p1);
-            p0 -= low_half(pf[kk][part][x]);
-            p1 -= high_half(pf[kk][part][x]);
+            const uint32_t y = pack2(p0, p1);
+            p0 -= low_half(y);
+            p1 -= high_half(y);
+            pf[n][part][x] = transpose8(y);
           }
         }
 #pragma unroll
-      for (int n4 = 0; n4 < HD / 32; ++n4) {
-        float y[4][4];
+      for (int d = 0; d < DB; ++d) {
+        uint32_t vf[4];
+        ldsm4t(vb + poff<HD>((lane & 7) + ((lane >> 4) << 3), d * 2 + ((lane >> 3) & 1)), vf);
+        float y[QN][4];
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+        for (int n = 0; n < QN; ++n)
 #pragma unroll
           for (int x = 0; x < 4; ++x) y[n][x] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < NT / 2; ++kk) {
-          uint32_t vf[2][4];
-          ldsm4t(vb + poff<HD>(kk * 16 + (lane & 15), n4 * 4 + (lane >> 4)), vf[0]);
-          ldsm4t(vb + poff<HD>(kk * 16 + (lane & 15), n4 * 4 + 2 + (lane >> 4)), vf[1]);
+        for (int part = 2; part >= 0; --part)
 #pragma unroll
-          for (int part = 2; part >= 0; --part)
+          for (int n = 0; n < QN; ++n) mma16816(y[n], vf, pf[n][part][0], pf[n][part][1]);
 #pragma unroll
-            for (int n = 0; n < 4; ++n) mma16816(y[n], pf[kk][part], vf[n >> 1][(n & 1) * 2], vf[n >> 1][(n & 1) * 2 + 1]);
-        }
+        for (int n = 0; n < QN; ++n)
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) o[4 * n4 + n][x] = fmaf(o[4 * n4 + n][x], corr[x >> 1], y[n][x]);
+          for (int x = 0; x < 4; ++x) o[n][d][x] = fmaf(o[n][d][x], corr[n][x & 1], y[n][x]);
       }
       stage = stage + 1 == S ? 0 : stage + 1;
     }
 
-    // ---- the warps' results: every warp adds up OWN column blocks
+    // ---- the warps' results, a block of queries at a time: warp w adds up element blocks w, w + W ..
 #pragma unroll
-    for (int hh = 0; hh < 2; ++hh) {
-      l_run[hh] += __shfl_xor_sync(0xffffffffu, l_run[hh], 1);
-      l_run[hh] += __shfl_xor_sync(0xffffffffu, l_run[hh], 2);
-    }
-    if (t4 == 0) { ml[warp][g4] = make_float2(m_run[0], l_run[0]); ml[warp][g4 + 8] = make_float2(m_run[1], l_run[1]); }
+    for (int n = 0; n < QN; ++n)
 #pragma unroll
-    for (int w = 0; w < W; ++w)
-      if (w != warp) {
-#pragma unroll
-        for (int n = 0; n < OWN; ++n)
-          exchange[((w * (W - 1) + (warp < w ? warp : warp - 1)) * OWN + n) * 32 + lane] =
-              make_float4(o[w * OWN + n][0], o[w * OWN + n][1], o[w * OWN + n][2], o[w * OWN + n][3]);
+      for (int x = 0; x < 2; ++x) {
+        l_run[n][x] += __shfl_xor_sync(0xffffffffu, l_run[n][x], 4);
+        l_run[n][x] += __shfl_xor_sync(0xffffffffu, l_run[n][x], 8);
+        l_run[n][x] += __shfl_xor_sync(0xffffffffu, l_run[n][x], 16);
+        if (g4 == 0) ml[warp][n * 8 + t4 * 2 + x] = make_float2(m_run[n][x], l_run[n][x]);
       }
-    __syncthreads();
-    float M[2], den[2], mine[2];
-#pragma unroll
-    for (int hh = 0; hh < 2; ++hh) {
-      float2 v[W];
-      M[hh] = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < W; ++w) { v[w] = ml[w][g4 + 8 * hh]; M[hh] = fmaxf(M[hh], v[w].x); }
-      den[hh] = 0.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) den[hh] = fmaf(v[w].y, v[w].x == -INFINITY && v[w].y == 0.f ? 0.f : ex2((v[w].x - M[hh]) * sl2), den[hh]);
-      mine[hh] = m_run[hh] == -INFINITY && l_run[hh] == 0.f ? 0.f : ex2((m_run[hh] - M[hh]) * sl2);
+    const bool whole = LINE ? seg_n == seg.k.n : gridDim.x == 1;
+    // where sums go that are not the whole unit's: scratch, or this CTA's shared memory (the ring, drained)
+    float *part = LINE ? a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * (Q * (HD + 2)) : reinterpret_cast<float *>(base_g);
+    if (!LINE) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncthreads();
     }
-    float sum[OWN][4];
 #pragma unroll
-    for (int w = 0; w < W; ++w)
-      if (w == warp) {
+    for (int n = 0; n < QN; ++n) {
+      if (n) __syncthreads();
 #pragma unroll
-        for (int n = 0; n < OWN; ++n)
+      for (int d = 0; d < DB; ++d)
+        if (d % W != warp) exchange[(d * (W - 1) + (warp < d % W ? warp : warp - 1)) * 32 + lane] = make_float4(o[n][d][0], o[n][d][1], o[n][d][2], o[n][d][3]);
+      __syncthreads();
+      float M[2], den[2];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) sum[n][x] = mine[x >> 1] * o[w * OWN + n][x];
-      }
+      for (int x = 0; x < 2; ++x) {
+        M[x] = -INFINITY;
+        den[x] = 0.f;
 #pragma unroll
-    for (int k = 0; k < W - 1; ++k) {
-      const int w = k < warp ? k : k + 1;
-      float f[2];
+        for (int w = 0; w < W; ++w) M[x] = fmaxf(M[x], ml[w][n * 8 + t4 * 2 + x].x);
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        const float2 v = ml[w][g4 + 8 * hh];
-        f[hh] = v.x == -INFINITY && v.y == 0.f ? 0.f : ex2((v.x - M[hh]) * sl2);
+        for (int w = 0; w < W; ++w) {
+          const float2 v = ml[w][n * 8 + t4 * 2 + x];
+          den[x] = fmaf(v.y, part_weight(v, M[x], sl2), den[x]);
+        }
       }
 #pragma unroll
-      for (int n = 0; n < OWN; ++n) {
-        const float4 x = exchange[((warp * (W - 1) + k) * OWN + n) * 32 + lane];
-        sum[n][0] = fmaf(f[0], x.x, sum[n][0]);
-        sum[n][1] = fmaf(f[0], x.y, sum[n][1]);
-        sum[n][2] = fmaf(f[1], x.z, sum[n][2]);
-        sum[n][3] = fmaf(f[1], x.w, sum[n][3]);
+      for (int k = 0; k < OWN; ++k) {
+        const int d = k * W + warp;
+        if (d >= DB) break;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < W; ++w) {
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (w != warp) x = exchange[(d * (W - 1) + (w < warp ? w : w - 1)) * 32 + lane];
+          else {
+#pragma unroll
+            for (int e = 0; e < DB; ++e)
+              if (e == d) x = make_float4(o[n][e][0], o[n][e][1], o[n][e][2], o[n][e][3]);
+          }
+          const float f0 = part_weight(ml[w][n * 8 + t4 * 2], M[0], sl2), f1 = part_weight(ml[w][n * 8 + t4 * 2 + 1], M[1], sl2);
+          sum[0] = fmaf(f0, x.x, sum[0]); sum[1] = fmaf(f1, x.y, sum[1]);
+          sum[2] = fmaf(f0, x.z, sum[2]); sum[3] = fmaf(f1, x.w, sum[3]);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int q = q0 + n * 8 + t4 * 2 + x;
+          if (q >= nq) continue;
+          const int j = q / group, h = seg.kvh * group + q - j * group;
+          const float f = !whole ? 1.f : seg.len < 0 ? 0.f : result_scale(a, pos[n][x], den[x]);
+          float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + (q - q0) * HD;
+          to[d * 16 + g4] = sum[x] * f;
+          to[d * 16 + g4 + 8] = sum[x + 2] * f;
+          if (!whole && d == 0 && g4 == 0) {
+            if (LINE) *reinterpret_cast<float2 *>(part + Q * HD + (q - q0) * 2) = make_float2(M[x], den[x]);
+            else ml_cta[q - q0] = make_float2(M[x], den[x]);
+          }
+        }
       }
     }
-    const bool whole = seg_n == seg.k.n;
-    float *part = a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * (16 * (HD + 2));
-#pragma unroll
-    for (int hh = 0; hh < 2; ++hh) {
-      const int q = q0 + g4 + hh * 8;
-      if (q >= nq) continue;
-      const int j = q / group, h = kvh * group + q - j * group;
-      const float f = whole ? result_scale(a, pos[hh], den[hh]) : 1.f;
-      float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + (g4 + hh * 8) * HD;
-#pragma unroll
-      for (int n = 0; n < OWN; ++n)
-        *reinterpret_cast<float2 *>(to + (warp * OWN + n) * 8 + t4 * 2) = make_float2(sum[n][2 * hh] * f, sum[n][2 * hh + 1] * f);
-      if (!whole && warp == 0 && t4 == 0) *reinterpret_cast<float2 *>(part + 16 * HD + (g4 + hh * 8) * 2) = make_float2(M[hh], den[hh]);
-    }
+    if (!LINE) break;
     done += seg_n;
     if (done == n_mine) break;
-    move_on(a, seg, seg_n);
+    bool unit;
+    move_on(a, seg, seg_n, unit);
     __syncthreads();                                     // the exchange buffers are free again
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
+  if (LINE) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    return;
+  }
+  if (gridDim.x == 1) return;
+  // ---- the cluster's parts: un-normalised sums and (max, sum) of each CTA in its shared memory
+  cluster_sync_all();
+  const int q0 = seg.qg * Q, rows = min(Q, nq - q0), ns = gridDim.x;
+  const uint32_t ml_addr = smem_u32(ml_cta);
+  for (int e = blockIdx.x * kThreads + tid; e < rows * (HD / 4); e += ns * kThreads) {
+    const int row = e / (HD / 4), c4 = e - row * (HD / 4);
+    float2 mv[8];
+    float4 ov[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      mv[r] = make_float2(-INFINITY, 0.f);
+      ov[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < ns) {
+        mv[r] = ld_cluster_f2(map_to_cta(ml_addr + (uint32_t)row * 8u, (uint32_t)r));
+        ov[r] = ld_cluster_f4(map_to_cta(base + (uint32_t)(row * HD + c4 * 4) * 4u, (uint32_t)r));
+      }
+    }
+    float M = -INFINITY, den = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) M = fmaxf(M, mv[r].x);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float f = part_weight(mv[r], M, sl2);
+      den = fmaf(mv[r].y, f, den);
+      acc.x = fmaf(f, ov[r].x, acc.x); acc.y = fmaf(f, ov[r].y, acc.y); acc.z = fmaf(f, ov[r].z, acc.z); acc.w = fmaf(f, ov[r].w, acc.w);
+    }
+    const int q = q0 + row, j = q / group, h = seg.kvh * group + q - j * group;
+    const float f = seg.len < 0 ? 0.f : result_scale(a, seg.len + j, den);
+    *reinterpret_cast<float4 *>(a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD + c4 * 4) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+  }
+  cluster_sync_all();                                    // the others may still be reading this CTA's memory
 }
 
 // ------------------------------------------------------------------------------------ joining the parts of a unit
 // One block per unit: with items = queries x hd / 4 pieces of four columns, threads are groups that take turns at the parts.
 constexpr int kCombine = 256;
 
-template <int HD>
+template <int HD, int QN>
 __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_constant__ PagedAttnArgs a, int workers) {
   __shared__ long long counts[2];
   __shared__ float4 acc_s[kCombine];
   __shared__ float2 ml_s[kCombine];
-  const int b = blockIdx.x / a.units, u = blockIdx.x - b * a.units, tid = threadIdx.x;
+  constexpr int Q = 8 * QN;
+  const int units = a.groups * a.pool.n_kv_heads, b = blockIdx.x / units, u = blockIdx.x - b * units, tid = threadIdx.x;
   int len;
   const KeyTiles k = seq_tiles(a, b, len);
   if (tid < 32) {
@@ -465,8 +554,8 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
     if (tid == 0) { counts[0] = total; counts[1] = before; }
   }
   __syncthreads();
-  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c, nqg = a.units / a.pool.n_kv_heads;
-  const int kvh = u / nqg, q0 = (u - kvh * nqg) * 16, n_rows = min(16, nq - q0), items = n_rows * (HD / 4);
+  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c;
+  const int kvh = u / a.groups, q0 = (u - kvh * a.groups) * Q, n_rows = min(Q, nq - q0), items = n_rows * (HD / 4);
   const long long chunk = chunk_of(counts[0], workers), begin = counts[1] + (long long)u * k.n;
   UnitParts w = {0, -1};
   if (k.n > 0) {
@@ -494,8 +583,8 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
           v[i] = make_float2(-INFINITY, 0.f);
           x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (at <= w.last) {
-            const float *part = a.parts + ((long long)at * 2 + part_place(begin, at, chunk)) * (16 * (HD + 2));
-            v[i] = __ldcg(reinterpret_cast<const float2 *>(part + 16 * HD + row * 2));
+            const float *part = a.parts + ((long long)at * 2 + part_place(begin, at, chunk)) * (Q * (HD + 2));
+            v[i] = __ldcg(reinterpret_cast<const float2 *>(part + Q * HD + row * 2));
             x[i] = __ldcg(reinterpret_cast<const float4 *>(part + row * HD + c4 * 4));
           }
         }
@@ -507,7 +596,7 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
         den *= f; acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-          const float s = v[i].x == -INFINITY && v[i].y == 0.f ? 0.f : ex2((v[i].x - top) * sl2);
+          const float s = part_weight(v[i], top, sl2);
           den = fmaf(v[i].y, s, den);
           acc.x = fmaf(s, x[i].x, acc.x); acc.y = fmaf(s, x[i].y, acc.y); acc.z = fmaf(s, x[i].z, acc.z); acc.w = fmaf(s, x[i].w, acc.w);
         }
@@ -520,12 +609,12 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
       if (g == 0) {
         float top = m;
         for (int i = 1; i < groups; ++i) top = fmaxf(top, ml_s[tid + i * items].x);
-        float f = m == -INFINITY && den == 0.f ? 0.f : ex2((m - top) * sl2);
+        float f = part_weight(make_float2(m, den), top, sl2);
         den *= f; acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
         for (int i = 1; i < groups; ++i) {
           const float2 v = ml_s[tid + i * items];
           const float4 x = acc_s[tid + i * items];
-          f = v.x == -INFINITY && v.y == 0.f ? 0.f : ex2((v.x - top) * sl2);
+          f = part_weight(v, top, sl2);
           den = fmaf(v.y, f, den);
           acc.x = fmaf(f, x.x, acc.x); acc.y = fmaf(f, x.y, acc.y); acc.z = fmaf(f, x.z, acc.z); acc.w = fmaf(f, x.w, acc.w);
         }
@@ -590,44 +679,69 @@ __global__ void __launch_bounds__(128) paged_fma_kernel(const __grid_constant__ 
 }
 
 // ------------------------------------------------------------------------------------ host side
-template <int HD>
-cudaError_t launch_mma(const PagedAttnArgs &a, int workers, cudaStream_t st) {
-  using C = PagedCfg<HD>;
-  static bool attr_done[kMaxDevices] = {false};
+template <typename K>
+cudaError_t allow_smem(K kernel, size_t bytes, bool *done) {
   const int dev = current_device_slot();
-  if (!attr_done[dev]) {
-    if (cudaError_t e = cudaFuncSetAttribute(paged_mma_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem)) return e;
-    attr_done[dev] = true;
-  }
-  paged_mma_kernel<HD><<<workers, C::W * 32, C::kSmem, st>>>(a);
+  if (done[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  done[dev] = e == cudaSuccess;
+  return e;
+}
+
+template <int HD, int QN>
+cudaError_t launch_line(const PagedAttnArgs &a, cudaStream_t st) {
+  using C = PagedCfg<HD>;
+  static bool done[kMaxDevices] = {false};
+  if (cudaError_t e = allow_smem(paged_mma_kernel<HD, QN, true>, C::kSmem, done)) return e;
+  paged_mma_kernel<HD, QN, true><<<kWorkers, kThreads, C::kSmem, st>>>(a);
   if (cudaError_t e = cudaGetLastError()) return e;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
-  cfg.gridDim = dim3((unsigned)(a.batch * a.units)); cfg.blockDim = dim3(kCombine); cfg.stream = st;
+  cfg.gridDim = dim3((unsigned)(a.batch * a.groups * a.pool.n_kv_heads)); cfg.blockDim = dim3(kCombine); cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, paged_combine_kernel<HD>, a, workers);
+  return cudaLaunchKernelEx(&cfg, paged_combine_kernel<HD, QN>, a, kWorkers);
 }
 
+template <int HD, int QN>
+cudaError_t launch_cluster(const PagedAttnArgs &a, int ctas, cudaStream_t st) {
+  using C = PagedCfg<HD>;
+  static bool done[kMaxDevices] = {false};
+  if (cudaError_t e = allow_smem(paged_mma_kernel<HD, QN, false>, C::kSmem, done)) return e;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = dim3(ctas, a.groups * a.pool.n_kv_heads, a.batch); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, paged_mma_kernel<HD, QN, false>, a);
+}
+
+template <int HD, int QN>
+cudaError_t launch_mma(PagedAttnArgs a, cudaStream_t st) {
+  const int nq = a.hq / a.pool.n_kv_heads * a.c;
+  a.groups = (nq + 8 * QN - 1) / (8 * QN);
+  const int ctas = paged_cluster(a.batch, a.groups * a.pool.n_kv_heads, a.cap, a.c, a.window, a.n_sink, kKeys, kWarps, kWorkers);
+  return ctas ? launch_cluster<HD, QN>(a, ctas, st) : launch_line<HD, QN>(a, st);
+}
 template <int HD>
-cudaError_t launch_fma(const PagedAttnArgs &a, cudaStream_t st) {
-  paged_fma_kernel<HD><<<dim3(a.batch * a.c, a.hq), 128, 0, st>>>(a);
-  return cudaGetLastError();
+cudaError_t launch_hd(const PagedAttnArgs &a, int dtype, cudaStream_t st) {
+  if (dtype == FC_F32) {
+    paged_fma_kernel<HD><<<dim3(a.batch * a.c, a.hq), 128, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  return a.hq / a.pool.n_kv_heads * a.c <= 8 ? launch_mma<HD, 1>(a, st) : launch_mma<HD, 2>(a, st);
 }
-
-constexpr int kWorkers = 148;
 
 }  // namespace
 
 size_t paged_attn_scratch(int hd, int dtype) { return dtype == FC_F32 ? 256 : (size_t)kWorkers * 2 * 16 * (hd + 2) * sizeof(float); }
 
-cudaError_t launch_paged_attn(PagedAttnArgs a, int dtype, int hd, cudaStream_t st) {
-  const int group = a.hq / a.pool.n_kv_heads;
-  a.units = a.pool.n_kv_heads * ((group * a.c + 15) / 16);
-  if (dtype == FC_F32) return hd == 128 ? launch_fma<128>(a, st) : hd == 64 ? launch_fma<64>(a, st) : launch_fma<32>(a, st);
-  return hd == 128 ? launch_mma<128>(a, kWorkers, st) : hd == 64 ? launch_mma<64>(a, kWorkers, st) : launch_mma<32>(a, kWorkers, st);
+cudaError_t launch_paged_attn(const PagedAttnArgs &a, int dtype, int hd, cudaStream_t st) {
+  return hd == 128 ? launch_hd<128>(a, dtype, st) : hd == 64 ? launch_hd<64>(a, dtype, st) : launch_hd<32>(a, dtype, st);
 }
 
 }  // namespace fc
