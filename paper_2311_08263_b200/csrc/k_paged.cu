@@ -84,6 +84,17 @@ PageView view_of(const fc_pages *p, int layer) {
   return v;
 }
 
+// Turns per position of the pairs.  64 powers are a microsecond, so a thread keeps those of the base and head size that it used last.
+void rope_turns(float theta, int hd, double *turns) {
+  struct Last { float theta; int hd; double turns[64]; };
+  static thread_local Last last = {0.f, 0, {0}};
+  if (last.theta != theta || last.hd != hd) {
+    for (int i = 0; i < hd / 2; ++i) last.turns[i] = std::pow((double)theta, -2.0 * i / hd) / 6.283185307179586476925286766559;
+    last.theta = theta; last.hd = hd;
+  }
+  memcpy(turns, last.turns, sizeof(double) * (hd / 2));
+}
+
 }  // namespace
 }  // namespace fc
 
@@ -100,7 +111,7 @@ extern "C" int fc_op_paged_store(const fc_pages *pages, int32_t layer, const int
   a.pool = view_of(pages, layer);
   a.table = table; a.width = table_width; a.kv_len = kv_len; a.qkv = qkv; a.qkv_stride = qkv_stride; a.q = q_out;
   a.c = c; a.hq = n_heads; a.hd = hd;
-  for (int i = 0; i < hd / 2; ++i) a.turns[i] = std::pow((double)rope_theta, -2.0 * i / hd) / 6.283185307179586476925286766559;
+  rope_turns(rope_theta, hd, a.turns);
   const int rows = batch * c, units = (n_heads + 2 * pages->n_kv_heads) * (hd >> 3);
   int ny = (4 * 148 + rows - 1) / rows;               // about four blocks per SM when there are few rows
   if (ny > (units + 255) / 256) ny = (units + 255) / 256;

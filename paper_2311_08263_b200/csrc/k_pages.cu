@@ -16,16 +16,18 @@ namespace fc {
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kListed = 512;            // table rows named in one launch's parameters
-struct SeqList { int n; int a[kListed], b[kListed]; };
+// Table rows named in one launch's parameters: a few, or many (large parameters cost the launch about a microsecond).
+constexpr int kListed = 500, kFew = 32;
+template <int N> struct SeqList { int a[N], b[N]; };
 
 // ------------------------------------------------------------------------------------------------ free, fork
 __device__ __forceinline__ void release(int32_t *refs, int n_pages, int e) {
   if (e >= 0 && e < n_pages) atomicSub(refs + e, 1);
 }
 
+template <int N>
 __global__ void __launch_bounds__(128) pages_free_kernel(int32_t *table, int width, int32_t *kv_len, int32_t *refs, int n_pages, int page_size,
-                                                        const __grid_constant__ SeqList list, int window, int n_sink) {
+                                                        const __grid_constant__ SeqList<N> list, int window, int n_sink) {
   const int s = list.a[blockIdx.x];
   int32_t *row = table + (long long)s * width;
   const int len = kv_len[s];
@@ -38,8 +40,9 @@ __global__ void __launch_bounds__(128) pages_free_kernel(int32_t *table, int wid
   if (window == 0 && threadIdx.x == 0) kv_len[s] = -1;
 }
 
+template <int N>
 __global__ void __launch_bounds__(128) pages_fork_kernel(int32_t *table, int width, int32_t *kv_len, int32_t *refs, int n_pages, int page_size,
-                                                        const __grid_constant__ SeqList list) {
+                                                        const __grid_constant__ SeqList<N> list) {
   const int src = list.a[blockIdx.x], dst = list.b[blockIdx.x];
   const int32_t *from = table + (long long)src * width;
   int32_t *to = table + (long long)dst * width;
@@ -109,6 +112,7 @@ __device__ __forceinline__ int held_page(const ReserveArgs &a, int b, int i) {
 }
 
 __global__ void __launch_bounds__(kPlanThreads) pages_reserve_kernel(const __grid_constant__ ReserveArgs a) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the copies wait until this is done
   const int tid = threadIdx.x;
   __shared__ int copies;
   if (tid == 0) copies = 0;
@@ -186,11 +190,12 @@ __global__ void __launch_bounds__(kPlanThreads) pages_reserve_kernel(const __gri
 // ------------------------------------------------------------------------------------------------ compact
 struct CompactArgs {
   int32_t *refs; int n_pages;
-  int32_t *n_live;
-  int32_t *dst, *src, *place, *n_moves;     // scratch: holes, pages that move, where each page from n on goes
+  int32_t *n_live;                          // of the caller, or null
+  int32_t *dst, *src, *place, *counts;      // scratch: holes, pages that move, where each page from n on goes; how many move, how many live
 };
 
 __global__ void __launch_bounds__(kPlanThreads) pages_compact_kernel(const __grid_constant__ CompactArgs a) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the copies wait until this is done
   const int tid = threadIdx.x;
   int live = 0, all;
   for (int p = tid; p < a.n_pages; p += kPlanThreads) live += a.refs[p] > 0;
@@ -217,7 +222,8 @@ __global__ void __launch_bounds__(kPlanThreads) pages_compact_kernel(const __gri
     a.refs[from] = 0;
   }
   if (tid == 0) {
-    *a.n_moves = high;
+    a.counts[0] = high;
+    a.counts[1] = n;
     if (a.n_live) *a.n_live = n;
   }
 }
@@ -240,6 +246,7 @@ struct CopyArgs {
 constexpr int kCopyThreads = 256, kCopyUnroll = 4;
 
 __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_constant__ CopyArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");                    // the kernel that decided what is copied
   const int n = *a.n;
   const unsigned int chunk = kCopyThreads * kCopyUnroll, chunks = (a.piece + chunk - 1) / chunk;
   const long long units = (long long)n * a.n_layers * 2 * chunks;
@@ -298,10 +305,14 @@ cudaError_t launch_copy(const fc_pages &p, CopyArgs a, cudaStream_t st) {
     if (inner == 1 || is == run) { run *= inner; inner = 1; is = 0; }
   }
   a.run = (unsigned int)run; a.inner = (unsigned int)inner; a.inner_stride = is; a.outer_stride = os;
-  int sms = 0;
-  if (cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, current_device_slot())) return e;
-  pages_copy_kernel<<<8 * sms, kCopyThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = dim3(8 * 148); cfg.blockDim = dim3(kCopyThreads); cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, pages_copy_kernel, a);
 }
 
 // ------------------------------------------------------------------------------------------------ arguments
@@ -320,6 +331,18 @@ struct Marks {
   ~Marks() { delete[] m; }
   bool once(int i) { if (i < 0 || i >= n || m[i]) return false; m[i] = 1; return true; }
 };
+
+// n named rows, a launch for every list that they fill.
+template <typename F>
+int by_lists(int n, F launch) {
+  for (int i0 = 0; i0 < n; i0 += kListed) {
+    const int count = n - i0 < kListed ? n - i0 : kListed;
+    if (count <= kFew) { SeqList<kFew> list; launch(list, i0, count); }
+    else { SeqList<kListed> list; launch(list, i0, count); }
+    if (cudaGetLastError() != cudaSuccess) return FC_ERR_CUDA;
+  }
+  return FC_OK;
+}
 
 }  // namespace
 
@@ -360,14 +383,10 @@ extern "C" int fc_op_pages_free(int32_t *table, int32_t table_width, int32_t n_s
   if (!marks.m) return FC_ERR_ARG;
   for (int i = 0; i < n; ++i)
     if (!marks.once(seqs[i])) return FC_ERR_ARG;
-  for (int i0 = 0; i0 < n; i0 += kListed) {
-    SeqList list;
-    list.n = n - i0 < kListed ? n - i0 : kListed;
-    memcpy(list.a, seqs + i0, list.n * sizeof(int));
-    pages_free_kernel<<<list.n, 128, 0, (cudaStream_t)cuda_stream>>>(table, table_width, kv_len, refs, n_pages, page_size, list, window, n_sink);
-    if (cudaGetLastError() != cudaSuccess) return FC_ERR_CUDA;
-  }
-  return FC_OK;
+  return by_lists(n, [&](auto &list, int i0, int count) {
+    memcpy(list.a, seqs + i0, count * sizeof(int));
+    pages_free_kernel<<<count, 128, 0, (cudaStream_t)cuda_stream>>>(table, table_width, kv_len, refs, n_pages, page_size, list, window, n_sink);
+  });
 }
 
 extern "C" int fc_op_pages_fork(int32_t *table, int32_t table_width, int32_t n_seqs, int32_t *kv_len, int32_t *refs, int32_t n_pages,
@@ -380,15 +399,11 @@ extern "C" int fc_op_pages_fork(int32_t *table, int32_t table_width, int32_t n_s
     if (!marks.once(dst[i])) return FC_ERR_ARG;
   for (int i = 0; i < n; ++i)
     if (src[i] < 0 || src[i] >= n_seqs || marks.m[src[i]]) return FC_ERR_ARG;
-  for (int i0 = 0; i0 < n; i0 += kListed) {
-    SeqList list;
-    list.n = n - i0 < kListed ? n - i0 : kListed;
-    memcpy(list.a, src + i0, list.n * sizeof(int));
-    memcpy(list.b, dst + i0, list.n * sizeof(int));
-    pages_fork_kernel<<<list.n, 128, 0, (cudaStream_t)cuda_stream>>>(table, table_width, kv_len, refs, n_pages, page_size, list);
-    if (cudaGetLastError() != cudaSuccess) return FC_ERR_CUDA;
-  }
-  return FC_OK;
+  return by_lists(n, [&](auto &list, int i0, int count) {
+    memcpy(list.a, src + i0, count * sizeof(int));
+    memcpy(list.b, dst + i0, count * sizeof(int));
+    pages_fork_kernel<<<count, 128, 0, (cudaStream_t)cuda_stream>>>(table, table_width, kv_len, refs, n_pages, page_size, list);
+  });
 }
 
 // Scratch of a reservation: three lists of pages, a list of copies, two of sequences, the number of copies.
@@ -431,12 +446,10 @@ extern "C" int fc_op_pages_compact(const fc_pages *pages, int32_t *table, int32_
   const size_t n = pages->n_pages;
   int32_t *s = (int32_t *)scratch;
   CompactArgs a;
-  a.refs = refs; a.n_pages = pages->n_pages; a.dst = s; a.src = s + n; a.place = s + 2 * n; a.n_moves = s + 3 * n; a.n_live = s + 3 * n + 1;
+  a.refs = refs; a.n_pages = pages->n_pages; a.dst = s; a.src = s + n; a.place = s + 2 * n; a.counts = s + 3 * n; a.n_live = n_live;
   pages_compact_kernel<<<1, kPlanThreads, 0, st>>>(a);
   if (cudaGetLastError() != cudaSuccess) return FC_ERR_CUDA;
   CopyArgs c; memset(&c, 0, sizeof c);
-  c.src = a.src; c.dst = a.dst; c.n = a.n_moves; c.table = table; c.entries = (long long)table_width * n_seqs; c.place = a.place; c.n_live = a.n_live;
-  if (launch_copy(*pages, c, st) != cudaSuccess) return FC_ERR_CUDA;
-  if (n_live && cudaMemcpyAsync(n_live, a.n_live, sizeof(int32_t), cudaMemcpyDeviceToDevice, st) != cudaSuccess) return FC_ERR_CUDA;
-  return FC_OK;
+  c.src = a.src; c.dst = a.dst; c.n = a.counts; c.table = table; c.entries = (long long)table_width * n_seqs; c.place = a.place; c.n_live = a.counts + 1;
+  return launch_copy(*pages, c, st) == cudaSuccess ? FC_OK : FC_ERR_CUDA;
 }

@@ -299,41 +299,44 @@ def fc_op_short_window_attention(qkv_acc: torch.Tensor, sumsq: torch.Tensor, rms
 # device and return; they can be captured into CUDA graphs.
 
 _CACHE_TYPES = {torch.float32: _l.FC_F32, torch.bfloat16: _l.FC_BF16}
+_POOL = ("k and v: fp32 or bf16 tensors of the same shape and strides on one CUDA device, adjacent elements, "
+         "[layers, pages, kv heads, slots, head size] (operations on one layer: without the first dimension)")
 
 
 def _pool(k: torch.Tensor, v: torch.Tensor, dims: int) -> _l.fc_pages:
-    shape, stride = k.shape, k.stride()
-    if len(shape) != dims or k.dtype not in _CACHE_TYPES or v.dtype != k.dtype or v.shape != shape or v.stride() != stride or stride[-1] != 1:
-        raise ValueError("k and v: fp32 or bf16 tensors of the same shape and strides, adjacent elements, "
-                         + ("[layers, " if dims == 5 else "[") + "pages, kv heads, slots, head size]")
-    if not k.is_cuda or v.device != k.device:
-        raise ValueError("k and v have to be on one CUDA device")
+    shape, stride, dtype = k.shape, k.stride(), _CACHE_TYPES.get(k.dtype)
+    if (dtype is None or len(shape) != dims or v.shape != shape or v.stride() != stride or v.dtype is not k.dtype or stride[-1] != 1
+            or not k.is_cuda or v.device != k.device):
+        raise ValueError(_POOL)
     if dims == 4:
-        shape, stride = (1, *shape), (0, *stride)
-    return _l.fc_pages(k.data_ptr(), v.data_ptr(), _CACHE_TYPES[k.dtype], *shape, *stride[:4])
+        return _l.fc_pages(k.data_ptr(), v.data_ptr(), dtype, 1, *shape, 0, stride[0], stride[1], stride[2])
+    return _l.fc_pages(k.data_ptr(), v.data_ptr(), dtype, *shape, *stride[:4])
 
 
-def _ints(dev, ndim: int, **tensors):
-    for name, t in tensors.items():
-        if t.dtype != torch.int32 or t.ndim != ndim or t.device != dev or not t.is_contiguous():
-            raise ValueError(f"{name}: contiguous int32 tensor of {ndim} dimension(s) on {dev}")
+def _ints(name: str, t: torch.Tensor, dims: int, dev) -> int:
+    if t.dtype is not torch.int32 or t.dim() != dims or not t.is_contiguous() or t.device != dev or not t.is_cuda:
+        raise ValueError(f"{name}: contiguous int32 tensor of {dims} dimension(s) on the pool's CUDA device")
+    return t.data_ptr()
 
 
-def _rows(dev, table, kv_len):
-    _ints(dev, 2, table=table)
-    if kv_len is not None:
-        _ints(dev, 1, kv_len=kv_len)
-        if kv_len.shape[0] != table.shape[0]:
-            raise ValueError("kv_len: one length per row of the table")
+def _lengths(kv_len: torch.Tensor, table: torch.Tensor, dev) -> int:
+    if kv_len.shape[0] != table.shape[0]:
+        raise ValueError("kv_len: one length per row of the table")
+    return _ints("kv_len", kv_len, 1, dev)
+
+
+def _list(ids):
+    return (C.c_int32 * len(ids))(*ids)
 
 
 def _enqueue(dev, where: str, fn, *args):
-    stream = torch.cuda.current_stream(dev).cuda_stream
-    if dev.index == torch.cuda.current_device():
-        rc = fn(*args, stream)
+    """The call on the device's current stream (by its number: the stream object costs two microseconds)."""
+    at = dev.index
+    if at == torch.cuda.current_device():
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(at))
     else:
-        with torch.cuda.device(dev):
-            rc = fn(*args, stream)
+        with torch.cuda.device(at):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(at))
     if rc != _l.FC_OK:
         raise FcError(rc, where)
 
@@ -343,14 +346,15 @@ def fc_op_paged_store(qkv: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table
     """QKV rows of one layer into pages.  qkv fp32 [B*c, (n_heads + 2 n_kv_heads) * hd], rows adjacent or not; k/v [pages, n_kv_heads,
     slots, hd]; table int32 [B, width]; kv_len int32 [B].  Returns the rotated queries [B*c, n_heads * hd] in the pool's type; those of
     table rows without a sequence are not written."""
-    lib, dev = _l.load(), k.device
-    pool = _pool(k, v, 4)
-    _rows(dev, table, kv_len)
-    B, hd = table.shape[0], k.shape[3]
-    if qkv.dtype != torch.float32 or qkv.device != dev or qkv.shape != (B * c, (n_heads + 2 * k.shape[1]) * hd) or qkv.stride(1) != 1:
+    pool, dev = _pool(k, v, 4), k.device
+    tab = _ints("table", table, 2, dev)
+    B, width = table.shape
+    hd = pool.head_dim
+    if (qkv.dtype is not torch.float32 or qkv.shape != (B * c, (n_heads + 2 * pool.n_kv_heads) * hd) or qkv.stride(1) != 1
+            or qkv.device != dev):
         raise ValueError("qkv: fp32 [B * c, (n_heads + 2 n_kv_heads) * head size] with adjacent elements, on the pool's device")
     q = torch.empty(B * c, n_heads * hd, dtype=k.dtype, device=dev)
-    _enqueue(dev, "fc_op_paged_store", lib.fc_op_paged_store, pool, 0, table.data_ptr(), table.shape[1], kv_len.data_ptr(), qkv.data_ptr(),
+    _enqueue(dev, "fc_op_paged_store", _l.load().fc_op_paged_store, pool, 0, tab, width, _lengths(kv_len, table, dev), qkv.data_ptr(),
              qkv.stride(0), q.data_ptr(), B, c, n_heads, rope_theta)
     return q
 
@@ -359,76 +363,66 @@ def fc_op_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tab
                           n_heads: int, window: int = 0, n_sink: int = 0) -> torch.Tensor:
     """Window attention of one layer over pages, optionally under a sliding window with sinks.  q [B*c, n_heads * hd] in the pool's type,
     rows adjacent or not; the rest as in fc_op_paged_store, the rows' own keys and values stored.  Returns fp32 [B*c, n_heads * hd]."""
-    lib, dev = _l.load(), k.device
-    pool = _pool(k, v, 4)
-    _rows(dev, table, kv_len)
-    B, hkv, hd = table.shape[0], k.shape[1], k.shape[3]
-    if q.dtype != k.dtype or q.device != dev or q.shape != (B * c, n_heads * hd) or q.stride(1) != 1:
+    pool, dev = _pool(k, v, 4), k.device
+    tab = _ints("table", table, 2, dev)
+    B, width = table.shape
+    hd = pool.head_dim
+    if q.dtype is not k.dtype or q.shape != (B * c, n_heads * hd) or q.stride(1) != 1 or q.device != dev:
         raise ValueError("q: [B * c, n_heads * head size] in the pool's type with adjacent elements, on the pool's device")
-    nbytes = lib.fc_op_paged_attention_scratch_bytes(B, c, n_heads, hkv, hd, pool.dtype)
-    scratch = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=dev)
+    lib = _l.load()
+    nbytes = lib.fc_op_paged_attention_scratch_bytes(B, c, n_heads, pool.n_kv_heads, hd, pool.dtype)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     out = torch.empty(B * c, n_heads * hd, dtype=torch.float32, device=dev)
-    _enqueue(dev, "fc_op_paged_attention", lib.fc_op_paged_attention, pool, 0, table.data_ptr(), table.shape[1], kv_len.data_ptr(),
-             q.data_ptr(), q.stride(0), out.data_ptr(), B, c, n_heads, window, n_sink, scratch.data_ptr(), nbytes)
+    _enqueue(dev, "fc_op_paged_attention", lib.fc_op_paged_attention, pool, 0, tab, width, _lengths(kv_len, table, dev), q.data_ptr(),
+             q.stride(0), out.data_ptr(), B, c, n_heads, window, n_sink, scratch.data_ptr(), nbytes)
     return out
-
-
-def _counted(table, kv_len, refs):
-    dev = table.device
-    if not table.is_cuda:
-        raise ValueError("table: on a CUDA device")
-    _rows(dev, table, kv_len)
-    _ints(dev, 1, refs=refs)
-    return dev
 
 
 def fc_op_pages_fork(table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, page_size: int, src, dst) -> None:
     """Table rows dst[i] share the pages of rows src[i]'s committed tokens (lists of row numbers on the host)."""
-    dev = _counted(table, kv_len, refs)
-    a, b = _i32(src), _i32(dst)
-    if a.shape != b.shape or a.ndim != 1:
+    dev, n = table.device, len(dst)
+    if len(src) != n:
         raise ValueError("src and dst: two lists of the same length")
-    _enqueue(dev, "fc_op_pages_fork", _l.load().fc_op_pages_fork, table.data_ptr(), table.shape[1], table.shape[0], kv_len.data_ptr(),
-             refs.data_ptr(), refs.shape[0], page_size, a.ctypes.data, b.ctypes.data, a.shape[0])
+    _enqueue(dev, "fc_op_pages_fork", _l.load().fc_op_pages_fork, _ints("table", table, 2, dev), table.shape[1], table.shape[0],
+             _lengths(kv_len, table, dev), _ints("refs", refs, 1, dev), refs.shape[0], page_size, _list(src), _list(dst), n)
 
 
 def fc_op_pages_free(table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, page_size: int, seqs, window: int = 0,
                      n_sink: int = 0) -> None:
     """Release the pages of table rows `seqs` (a list on the host): all of them, or those that no later row of a sliding window sees."""
-    dev = _counted(table, kv_len, refs)
-    a = _i32(seqs)
-    if a.ndim != 1:
-        raise ValueError("seqs: a list")
-    _enqueue(dev, "fc_op_pages_free", _l.load().fc_op_pages_free, table.data_ptr(), table.shape[1], table.shape[0], kv_len.data_ptr(),
-             refs.data_ptr(), refs.shape[0], page_size, a.ctypes.data, a.shape[0], window, n_sink)
+    dev = table.device
+    _enqueue(dev, "fc_op_pages_free", _l.load().fc_op_pages_free, _ints("table", table, 2, dev), table.shape[1], table.shape[0],
+             _lengths(kv_len, table, dev), _ints("refs", refs, 1, dev), refs.shape[0], page_size, _list(seqs), len(seqs), window, n_sink)
 
 
 def fc_op_pages_reserve(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor,
                         rows: int) -> torch.Tensor:
     """Pages for positions kv_len .. kv_len + rows - 1 of every sequence, copies of shared ones.  k/v [layers, pages, n_kv_heads, slots, hd].
     Returns int32 [n_seqs]: 1 where the positions can be written."""
-    lib, dev = _l.load(), k.device
-    pool = _pool(k, v, 5)
-    if _counted(table, kv_len, refs) != dev or refs.shape[0] != k.shape[1]:
-        raise ValueError("refs: one count per page, everything on the pool's device")
-    n = table.shape[0]
-    nbytes = lib.fc_op_pages_reserve_scratch_bytes(refs.shape[0], n)
+    pool, dev = _pool(k, v, 5), k.device
+    tab, counts = _ints("table", table, 2, dev), _ints("refs", refs, 1, dev)
+    n, width = table.shape
+    if refs.shape[0] != pool.n_pages:
+        raise ValueError("refs: one count per page")
+    lib = _l.load()
+    nbytes = lib.fc_op_pages_reserve_scratch_bytes(pool.n_pages, n)
     scratch = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     served = torch.empty(n, dtype=torch.int32, device=dev)
-    _enqueue(dev, "fc_op_pages_reserve", lib.fc_op_pages_reserve, pool, table.data_ptr(), table.shape[1], n, kv_len.data_ptr(),
-             refs.data_ptr(), rows, served.data_ptr(), scratch.data_ptr(), nbytes)
+    _enqueue(dev, "fc_op_pages_reserve", lib.fc_op_pages_reserve, pool, tab, width, n, _lengths(kv_len, table, dev), counts, rows,
+             served.data_ptr(), scratch.data_ptr(), nbytes)
     return served
 
 
 def fc_op_pages_compact(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, refs: torch.Tensor) -> torch.Tensor:
     """Move the pages in use to the front of the pool, in all layers; table and refs follow.  Returns int32 [1]: how many are in use."""
-    lib, dev = _l.load(), k.device
-    pool = _pool(k, v, 5)
-    if _counted(table, None, refs) != dev or refs.shape[0] != k.shape[1]:
-        raise ValueError("refs: one count per page, everything on the pool's device")
-    nbytes = lib.fc_op_pages_compact_scratch_bytes(refs.shape[0])
+    pool, dev = _pool(k, v, 5), k.device
+    tab, counts = _ints("table", table, 2, dev), _ints("refs", refs, 1, dev)
+    if refs.shape[0] != pool.n_pages:
+        raise ValueError("refs: one count per page")
+    lib = _l.load()
+    nbytes = lib.fc_op_pages_compact_scratch_bytes(pool.n_pages)
     scratch = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     n_live = torch.empty(1, dtype=torch.int32, device=dev)
-    _enqueue(dev, "fc_op_pages_compact", lib.fc_op_pages_compact, pool, table.data_ptr(), table.shape[1], table.shape[0], refs.data_ptr(),
-             n_live.data_ptr(), scratch.data_ptr(), nbytes)
+    _enqueue(dev, "fc_op_pages_compact", lib.fc_op_pages_compact, pool, tab, table.shape[1], table.shape[0], counts, n_live.data_ptr(),
+             scratch.data_ptr(), nbytes)
     return n_live

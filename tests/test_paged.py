@@ -142,7 +142,7 @@ def test_binding_refuses_tensors_that_do_not_fit():
     k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
     table, lens, refs = torch.zeros(1, 3, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
     q = torch.zeros(1, 2 * 64, dtype=torch.bfloat16)
-    with pytest.raises(ValueError, match="CUDA device"):
+    with pytest.raises(ValueError, match="one CUDA device"):
         engine.fc_op_paged_attention(q, k, k.clone(), table, lens, 1, 2)
     with pytest.raises(ValueError, match="same shape and strides"):
         engine.fc_op_paged_attention(q, k, k.float(), table, lens, 1, 2)
