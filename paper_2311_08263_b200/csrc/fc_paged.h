@@ -27,6 +27,7 @@ struct PagedAttnArgs {
   int batch, c, hq, window, n_sink;       // n_sink is 0 without a window
   int groups;             // groups of queries of a kv head (set by the launcher)
   float *parts;           // scratch: two parts per worker, [queries][hd] sums and [queries] (max, sum)
+  unsigned int *status;   // scratch of the kernel that has waits, else null: per worker, 1 where a wait ran out
 };
 
 // Length of a sequence as the kernels use it: -1 for none, never far beyond the table's `cap` positions (no sum overflows).
@@ -87,5 +88,8 @@ inline int paged_cluster(int batch, int units, int cap, int c, int window, int n
   while (ctas < 8 && tiles > ctas * warps && (long long)batch * units * ctas * 2 <= sms - 20) ctas *= 2;
   return (long long)batch * units * ctas <= sms && tiles <= 4ll * warps * ctas ? ctas : 0;
 }
+
+// Whether the kernel on tcgen05 takes a kv head's nq queries.
+inline bool paged_umma(int nq, int hd) { return nq > 32 && hd >= 64; }
 
 }  // namespace fc

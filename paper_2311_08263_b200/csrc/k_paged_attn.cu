@@ -14,12 +14,7 @@
 //
 // Probabilities enter the tensor cores as three bf16 parts (their sum has all 24 bits), a tile's product is added to the output in fp32: what is rounded
 // is what is stored in the cache, nothing else.  (Two parts leave 1.5e-6, relative, of the result.)
-#include <cstring>
-
-#include "fc_attn.cuh"
-#include "fc_internal.h"
-#include "fc_paged.h"
-#include "fc_ptx.cuh"
+#include "fc_paged.cuh"
 
 namespace fc {
 
@@ -27,7 +22,6 @@ namespace {
 
 constexpr int kKeys = 16;              // keys per tile
 constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kWorkers = 148;          // CTAs on the line: one per SM
 
 template <int HD>
 struct PagedCfg {
@@ -46,108 +40,12 @@ __device__ __forceinline__ uint32_t poff(int r, int ch) {
   if (HD == 32) return (uint32_t)r * 64u + (uint32_t)((ch ^ ((r >> 1) & 3)) << 4);
   return (uint32_t)(ch >> 3) * (kKeys * 128u) + (uint32_t)r * 128u + (uint32_t)(((ch & 7) ^ (r & 7)) << 4);
 }
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 // 8 x 8 transpose of 16-bit elements across a warp
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// What a part with maximum m and sum l counts against a maximum M; one that saw nothing counts nothing.
-__device__ __forceinline__ float part_weight(float2 part, float M, float sl2) {
-  return part.x == -INFINITY && part.y == 0.f ? 0.f : ex2((part.x - M) * sl2);
-}
-__device__ __forceinline__ float quiet_nan() { return __int_as_float(0x7fffffff); }
-
-__device__ __forceinline__ KeyTiles seq_tiles(const PagedAttnArgs &a, int b, int &len) {
-  len = clamp_len(a.kv_len[b], a.cap);
-  return key_tiles(len, a.c, a.cap, a.window, a.n_sink, kKeys);
-}
-
-// A place on the line of tiles: tile t of a unit (kv head, group of queries) of sequence b.
-struct Place {
-  int b, kvh, qg, t, len;
-  KeyTiles k;
-};
-// `step` tiles on; false behind the last one.  *unit: whether another unit is reached.
-__device__ __forceinline__ void move_on(const PagedAttnArgs &a, Place &p, int step, bool &unit) {
-  p.t += step;
-  unit = p.t >= p.k.n;
-  while (p.t >= p.k.n) {
-    p.t -= p.k.n;
-    if (++p.qg == a.groups) {
-      p.qg = 0;
-      if (++p.kvh == a.pool.n_kv_heads) {
-        p.kvh = 0;
-        do {
-          if (++p.b >= a.batch) { p.k.n = 0x7fffffff; return; }
-          p.k = seq_tiles(a, p.b, p.len);
-        } while (p.k.n == 0);
-      }
-    }
-  }
-}
-
-// Tiles of the whole call, and of the sequences in front of sequence `upto` (a warp does this together).
-__device__ __forceinline__ void count_tiles(const PagedAttnArgs &a, int upto, long long &total, long long &before) {
-  const int lane = threadIdx.x & 31, units = a.groups * a.pool.n_kv_heads;
-  long long all = 0, some = 0;
-  for (int b = lane; b < a.batch; b += 32) {
-    int len;
-    const long long n = (long long)seq_tiles(a, b, len).n * units;
-    all += n;
-    if (b < upto) some += n;
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    all += __shfl_xor_sync(0xffffffffu, all, o);
-    some += __shfl_xor_sync(0xffffffffu, some, o);
-  }
-  total = all;
-  before = some;
-}
-// The place of tile f of the line (a warp together; f is inside the line).
-__device__ __forceinline__ Place find_place(const PagedAttnArgs &a, long long f) {
-  const int lane = threadIdx.x & 31, units = a.groups * a.pool.n_kv_heads;
-  long long base = 0;
-  Place p = {0, 0, 0, 0, -1, {0, 0, 0}};
-  for (int b0 = 0; b0 < a.batch; b0 += 32) {
-    int len = -1;
-    KeyTiles k = {0, 0, 0};
-    if (b0 + lane < a.batch) k = seq_tiles(a, b0 + lane, len);
-    long long x = (long long)k.n * units;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    const unsigned int beyond = __ballot_sync(0xffffffffu, base + x > f);
-    if (beyond) {
-      const int w = __ffs(beyond) - 1;
-      p.k.n = __shfl_sync(0xffffffffu, k.n, w);
-      p.k.sinks = __shfl_sync(0xffffffffu, k.sinks, w);
-      p.k.first = __shfl_sync(0xffffffffu, k.first, w);
-      p.len = __shfl_sync(0xffffffffu, len, w);
-      p.b = b0 + w;
-      const long long at = f - (base + __shfl_sync(0xffffffffu, x, w) - (long long)p.k.n * units);
-      const int u = (int)(at / p.k.n);
-      p.t = (int)(at - (long long)u * p.k.n);
-      p.kvh = u / a.groups;
-      p.qg = u - p.kvh * a.groups;
-      return p;
-    }
-    base += __shfl_sync(0xffffffffu, x, 31);
-  }
-  return p;
-}
-
-// Result of a query: un-normalised sums over `den`.  A row that sees nothing is 0, one beyond the table NaN.
-__device__ __forceinline__ float result_scale(const PagedAttnArgs &a, int pos, float den) {
-  return pos >= a.cap ? quiet_nan() : den == 0.f ? 0.f : 1.0f / den;
-}
-
 // QN: blocks of 8 queries of a unit.  LINE: the line of tiles, else a cluster per unit (grid: CTAs of the cluster, units, sequences).
 template <int HD, int QN, bool LINE>
 __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_constant__ PagedAttnArgs a) {
@@ -173,14 +71,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
   int n_mine;
   if (LINE) {
     long long total, unused;
-    count_tiles(a, 0, total, unused);
+    count_tiles<kKeys>(a, 0, total, unused);
     const long long chunk = chunk_of(total, gridDim.x), f0 = chunk * blockIdx.x;
     if (f0 >= total) return;
     n_mine = (int)(total - f0 < chunk ? total - f0 : chunk);
-    seg = find_place(a, f0);
+    seg = find_place<kKeys>(a, f0);
   } else {
     seg.b = blockIdx.z; seg.kvh = blockIdx.y / a.groups; seg.qg = blockIdx.y - seg.kvh * a.groups;
-    seg.k = seq_tiles(a, seg.b, seg.len);
+    seg.k = seq_tiles<kKeys>(a, seg.b, seg.len);
     const int cut = (seg.k.n + gridDim.x - 1) / gridDim.x;
     seg.t = cut * blockIdx.x;
     n_mine = max(0, min(cut, seg.k.n - seg.t));
@@ -189,33 +87,34 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
   // ---- what is requested next: a tile of 16 keys, the lanes' keys (twice) looked up a tile ahead of the copies
   Place ld = seg;
   int ld_i = warp, see_from = 0, see_to = -1;            // keys that some query of the unit sees: the sinks, and from .. to
-  long long next_off = -1;
-  unsigned int next_bad = 0;
+  constexpr int kUnseen = -2;                            // a key that no query sees; -1: the table has no page for it
+  int next_page = kUnseen, next_slot = 0;                // page and slot of the lane's key: used a tile later, when they have arrived
   auto unit_keys = [&]() {
     see_from = window_first(ld.len + ld.qg * Q / group, a.window);                       // the first row's window reaches furthest back
     see_to = min(ld.len + min(nq - 1, ld.qg * Q + Q - 1) / group, a.cap - 1);
   };
   auto look_up = [&]() {
     const int t = tile_key(ld.k, ld.t, kKeys) + (lane & 15);
-    next_off = -1;
-    bool bad = false;
+    next_page = kUnseen;
     if (t <= see_to && (t >= see_from || t < a.n_sink)) {
-      const int i = t / a.pool.page_size, page = a.table[(long long)ld.b * a.width + i];
-      bad = page < 0 || page >= a.pool.n_pages;
-      if (!bad) next_off = (long long)page * a.pool.page_stride + (long long)(t - i * a.pool.page_size) * a.pool.slot_stride;
+      const int i = t / a.pool.page_size;
+      next_slot = t - i * a.pool.page_size;
+      next_page = max(-1, a.table[(long long)ld.b * a.width + i]);
     }
-    next_bad = __ballot_sync(0xffffffffu, bad) & 0xffffu;
   };
   auto request = [&](int stage) {
     if (ld_i < n_mine) {
-      if (lane == 0) bad_keys[warp][stage] = next_bad;
+      const bool there = next_page >= 0 && next_page < a.pool.n_pages;
+      const long long off = there ? (long long)next_page * a.pool.page_stride + (long long)next_slot * a.pool.slot_stride : -1;
+      const unsigned int bad = __ballot_sync(0xffffffffu, !there && next_page != kUnseen) & 0xffffu;
+      if (lane == 0) bad_keys[warp][stage] = bad;
       const uint32_t kb = ring + stage * C::kTile;
       const __nv_bfloat16 *k0 = (const __nv_bfloat16 *)a.pool.k + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
       const __nv_bfloat16 *v0 = (const __nv_bfloat16 *)a.pool.v + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
 #pragma unroll
       for (int i = 0; i < kKeys / RPI; ++i) {
         const int r = i * RPI + lane / PER;
-        const long long o = __shfl_sync(0xffffffffu, next_off, r);
+        const long long o = __shfl_sync(0xffffffffu, off, r);
         const uint32_t d = kb + poff<HD>(r, lane % PER), bytes = o < 0 ? 0u : 16u;      // keys that no row sees become zeros
         copy16(d, k0 + (o < 0 ? 0 : o), bytes);
         copy16(d + C::kHalf, v0 + (o < 0 ? 0 : o), bytes);
@@ -223,9 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
       ld_i += W;
       if (ld_i < n_mine) {
         if (LINE) {
-          bool unit;
-          move_on(a, ld, W, unit);
-          if (unit) unit_keys();
+          if (move_on<kKeys>(a, ld, W)) unit_keys();
         } else {
           ld.t += W;
         }
@@ -235,9 +132,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   if (ld_i < n_mine) {
-    bool unit;
-    if (!LINE) ld.t += warp;
-    else if (warp) move_on(a, ld, warp, unit);
+    if (LINE) move_on<kKeys>(a, ld, warp);
+    else ld.t += warp;
     unit_keys();
     look_up();
   }
@@ -492,8 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
     if (!LINE) break;
     done += seg_n;
     if (done == n_mine) break;
-    bool unit;
-    move_on(a, seg, seg_n, unit);
+    move_on<kKeys>(a, seg, seg_n);
     __syncthreads();                                     // the exchange buffers are free again
   }
   if (LINE) {
@@ -533,99 +428,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
     *reinterpret_cast<float4 *>(a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD + c4 * 4) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
   }
   cluster_sync_all();                                    // the others may still be reading this CTA's memory
-}
-
-// ------------------------------------------------------------------------------------ joining the parts of a unit
-// One block per unit: with items = queries x hd / 4 pieces of four columns, threads are groups that take turns at the parts.
-constexpr int kCombine = 256;
-
-template <int HD, int QN>
-__global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_constant__ PagedAttnArgs a, int workers) {
-  __shared__ long long counts[2];
-  __shared__ float4 acc_s[kCombine];
-  __shared__ float2 ml_s[kCombine];
-  constexpr int Q = 8 * QN;
-  const int units = a.groups * a.pool.n_kv_heads, b = blockIdx.x / units, u = blockIdx.x - b * units, tid = threadIdx.x;
-  int len;
-  const KeyTiles k = seq_tiles(a, b, len);
-  if (tid < 32) {
-    long long total, before;
-    count_tiles(a, b, total, before);
-    if (tid == 0) { counts[0] = total; counts[1] = before; }
-  }
-  __syncthreads();
-  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c;
-  const int kvh = u / a.groups, q0 = (u - kvh * a.groups) * Q, n_rows = min(Q, nq - q0), items = n_rows * (HD / 4);
-  const long long chunk = chunk_of(counts[0], workers), begin = counts[1] + (long long)u * k.n;
-  UnitParts w = {0, -1};
-  if (k.n > 0) {
-    w = unit_parts(begin, k.n, chunk);
-    if (w.first == w.last) return;                       // written by its one CTA
-  }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
-  int groups = 1;
-  while (groups * 2 * items <= kCombine) groups *= 2;
-  const int g = items <= kCombine ? tid / items : 0;
-  for (int e0 = 0; e0 < items; e0 += kCombine) {
-    const int e = items <= kCombine ? tid - g * items : e0 + tid;
-    const int row = e / (HD / 4), c4 = e - row * (HD / 4);
-    float m = -INFINITY, den = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (e < items && g < groups) {
-      constexpr int U = 4;
-      for (int p = w.first + g; p <= w.last; p += groups * U) {
-        float2 v[U];
-        float4 x[U];
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int at = p + i * groups;
-          v[i] = make_float2(-INFINITY, 0.f);
-          x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (at <= w.last) {
-            const float *part = a.parts + ((long long)at * 2 + part_place(begin, at, chunk)) * (Q * (HD + 2));
-            v[i] = __ldcg(reinterpret_cast<const float2 *>(part + Q * HD + row * 2));
-            x[i] = __ldcg(reinterpret_cast<const float4 *>(part + row * HD + c4 * 4));
-          }
-        }
-        float top = m;
-#pragma unroll
-        for (int i = 0; i < U; ++i) top = fmaxf(top, v[i].x);
-        const float f = m == top ? 1.f : ex2((m - top) * sl2);
-        m = top;
-        den *= f; acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const float s = part_weight(v[i], top, sl2);
-          den = fmaf(v[i].y, s, den);
-          acc.x = fmaf(s, x[i].x, acc.x); acc.y = fmaf(s, x[i].y, acc.y); acc.z = fmaf(s, x[i].z, acc.z); acc.w = fmaf(s, x[i].w, acc.w);
-        }
-      }
-    }
-    if (groups > 1) {
-      acc_s[tid] = acc;
-      ml_s[tid] = make_float2(m, den);
-      __syncthreads();
-      if (g == 0) {
-        float top = m;
-        for (int i = 1; i < groups; ++i) top = fmaxf(top, ml_s[tid + i * items].x);
-        float f = part_weight(make_float2(m, den), top, sl2);
-        den *= f; acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
-        for (int i = 1; i < groups; ++i) {
-          const float2 v = ml_s[tid + i * items];
-          const float4 x = acc_s[tid + i * items];
-          f = part_weight(v, top, sl2);
-          den = fmaf(v.y, f, den);
-          acc.x = fmaf(f, x.x, acc.x); acc.y = fmaf(f, x.y, acc.y); acc.z = fmaf(f, x.z, acc.z); acc.w = fmaf(f, x.w, acc.w);
-        }
-      }
-    }
-    if (e < items && g == 0) {
-      const int q = q0 + row, j = q / group, h = kvh * group + q - j * group;
-      const float f = len < 0 ? 0.f : result_scale(a, len + j, den);
-      *reinterpret_cast<float4 *>(a.out + (((long long)b * a.c + j) * a.hq + h) * HD + c4 * 4) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-    }
-  }
 }
 
 // ------------------------------------------------------------------------------------ fp32: a block per row and query head
@@ -679,15 +481,6 @@ __global__ void __launch_bounds__(128) paged_fma_kernel(const __grid_constant__ 
 }
 
 // ------------------------------------------------------------------------------------ host side
-template <typename K>
-cudaError_t allow_smem(K kernel, size_t bytes, bool *done) {
-  const int dev = current_device_slot();
-  if (done[dev]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  done[dev] = e == cudaSuccess;
-  return e;
-}
-
 template <int HD, int QN>
 cudaError_t launch_line(const PagedAttnArgs &a, cudaStream_t st) {
   using C = PagedCfg<HD>;
@@ -695,14 +488,7 @@ cudaError_t launch_line(const PagedAttnArgs &a, cudaStream_t st) {
   if (cudaError_t e = allow_smem(paged_mma_kernel<HD, QN, true>, C::kSmem, done)) return e;
   paged_mma_kernel<HD, QN, true><<<kWorkers, kThreads, C::kSmem, st>>>(a);
   if (cudaError_t e = cudaGetLastError()) return e;
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof cfg);
-  cfg.gridDim = dim3((unsigned)(a.batch * a.groups * a.pool.n_kv_heads)); cfg.blockDim = dim3(kCombine); cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, paged_combine_kernel<HD, QN>, a, kWorkers);
+  return launch_combine<HD, 8 * QN, kKeys>(a, kWorkers, st);
 }
 
 template <int HD, int QN>
@@ -733,12 +519,17 @@ cudaError_t launch_hd(const PagedAttnArgs &a, int dtype, cudaStream_t st) {
     paged_fma_kernel<HD><<<dim3(a.batch * a.c, a.hq), 128, 0, st>>>(a);
     return cudaGetLastError();
   }
-  return a.hq / a.pool.n_kv_heads * a.c <= 8 ? launch_mma<HD, 1>(a, st) : launch_mma<HD, 2>(a, st);
+  const int nq = a.hq / a.pool.n_kv_heads * a.c;
+  if (paged_umma(nq, HD)) return launch_paged_umma(a, HD, st);
+  return nq <= 8 ? launch_mma<HD, 1>(a, st) : launch_mma<HD, 2>(a, st);
 }
 
 }  // namespace
 
-size_t paged_attn_scratch(int hd, int dtype) { return dtype == FC_F32 ? 256 : (size_t)kWorkers * 2 * 16 * (hd + 2) * sizeof(float); }
+size_t paged_attn_scratch(int nq, int hd, int dtype) {
+  if (dtype == FC_F32) return 256;
+  return paged_umma(nq, hd) ? paged_umma_scratch(hd) : (size_t)kWorkers * 2 * 16 * (hd + 2) * sizeof(float);
+}
 
 cudaError_t launch_paged_attn(const PagedAttnArgs &a, int dtype, int hd, cudaStream_t st) {
   return hd == 128 ? launch_hd<128>(a, dtype, st) : hd == 64 ? launch_hd<64>(a, dtype, st) : launch_hd<32>(a, dtype, st);

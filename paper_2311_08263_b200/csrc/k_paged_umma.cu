@@ -1,0 +1,462 @@
+// Window attention over pages for many queries per kv head (windows of rows on grouped heads), on tcgen05: bf16, hd 64 / 128.
+//
+// A unit is a kv head of a sequence and 128 queries, the rows of the MMAs: S = Q.K^T (128 x 64 keys) and O = P.V (128 x hd), both operands
+// of the first and V of the second in shared memory, P in tensor memory.  The line of tiles, here of 64 keys, and the joining of parts are those of
+// k_paged_attn.cu.  One CTA per SM, three groups of four warps:
+//   softmax (two groups): the groups take turns at the tiles.  A thread owns a query: its scores come out of tensor memory in one piece, so that maximum
+//     and sum need no exchange; probabilities go back over the scores as three bf16 parts (all 24 bits), and the product of a tile is
+//     added to the thread's output in fp32 (the tensor core's own additions are not rounded to nearest).  While one group does this the tensor core works for
+//     the other.  Where a segment ends, the groups join through shared memory.
+//   the third: one thread issues the MMAs, three warps look up pages and load tiles (cp.async), one tile each in turn, and the queries of a
+//     unit in front of its first tile.
+// Every wait is bounded: where one runs out the CTA says so in its status word, and the joining kernel writes NaN for what it was to compute.
+//
+// Bound at hd 64 by HBM, the exponentials and the instruction issue alike (a tile: 700, 512 and about 1000 cycles), at hd 128 by the tensor core
+// (a tile's four products: 1024).
+#include "fc_paged.cuh"
+
+namespace fc {
+
+namespace {
+
+constexpr int kKeys = 64, kQueries = 128;
+constexpr int kThreads = 384;
+constexpr int kSoftRegs = 224, kLoadRegs = 56;           // registers a thread: 256 x 224 + 128 x 56 = 384 x 168, what the launch holds
+constexpr int kLoaders = 3;
+
+template <int HD>
+struct UmmaCfg {
+  static constexpr int SUB = HD / 64;                              // sub-tiles of 64 elements (128 bytes a row)
+  static constexpr uint32_t kSub = kKeys * 128u, kHalf = SUB * kSub, kTile = 2 * kHalf;
+  static constexpr int S = HD == 64 ? 8 : 4;                       // 128 KB of tiles
+  static constexpr uint32_t kQSub = kQueries * 128u, kQ = SUB * kQSub;
+  static constexpr uint32_t kExchange = kQueries * 64 * 4;         // 64 columns of the output at a time
+  static constexpr size_t kSmem = 1024 + (size_t)S * kTile + 2 * kQ + kExchange;
+};
+
+// 16-byte piece `ch` of row `r` in a tile of `rows` rows: rows of 128 bytes, the 128-byte swizzle of the MMA's operands.
+__device__ __forceinline__ uint32_t uoff(int rows, int r, int ch) {
+  return (uint32_t)(ch >> 3) * (uint32_t)rows * 128u + (uint32_t)r * 128u + (uint32_t)(((ch & 7) ^ (r & 7)) << 4);
+}
+// V as the B operand [hd x keys]: elements (N) adjacent, blocks of 64 of them a sub-tile apart, groups of eight keys 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_v(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)((kKeys * 128u) >> 4) << 16;
+  d |= (uint64_t)(1024u >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+// A in tensor memory
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(acc) : "memory");
+}
+// 32 columns of this thread's lane; the values are there after tmem_ld_done
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *v) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr) : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_constant__ PagedAttnArgs a) {
+  using C = UmmaCfg<HD>;
+  constexpr int S = C::S, PER = HD / 8;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) unsigned long long full[S], empty[S], q_free[2], s_ready[2], p_ready[2], o_ready[2], ex_full, ex_free, drained, odd_bar[2];
+  __shared__ unsigned int tmem_base_s, bad_keys[S][2], odd_keys[2][2];
+  __shared__ int gave_up;
+  __shared__ float2 ml[kQueries];
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  unsigned char *base_g = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t q_base = base + S * C::kTile;
+  float4 *exchange = reinterpret_cast<float4 *>(base_g + S * C::kTile + 2 * C::kQ);      // piece c4 of row r at r * 16 + (c4 ^ (r & 15))
+
+  long long total, unused;
+  count_tiles<kKeys>(a, 0, total, unused);
+  const long long chunk = chunk_of(total, gridDim.x), f0 = chunk * blockIdx.x;
+  if (f0 >= total) return;
+  const int n_mine = (int)(total - f0 < chunk ? total - f0 : chunk);
+  Place seg = find_place<kKeys>(a, f0);
+
+  if (tid == 0) {
+    for (int i = 0; i < S; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&q_free[i]), 1); mbar_init(smem_u32(&s_ready[i]), 1); mbar_init(smem_u32(&o_ready[i]), 1);
+      mbar_init(smem_u32(&p_ready[i]), 128); mbar_init(smem_u32(&odd_bar[i]), 128);
+      odd_keys[i][0] = odd_keys[i][1] = 0u;
+    }
+    mbar_init(smem_u32(&ex_full), 128); mbar_init(smem_u32(&ex_free), 128); mbar_init(smem_u32(&drained), 1);
+    gave_up = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+  }
+  if (warp == 8) tmem_alloc(smem_u32(&tmem_base_s), 512);
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_s;                     // group w: scores, then the parts of P, at column 256 w; the product at 256 w + 128
+  volatile int *quit = &gave_up;
+  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c;
+  const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
+    if (warp == 8) {
+      // ------------------------------------------------------------------------------------------ MMAs
+      if (lane == 0) {
+        constexpr uint32_t id_s = make_idesc(kKeys), id_o = make_idesc(HD) | (1u << 16);       // V: N adjacent
+        Place at = seg;
+        int so = 0;                                      // ordinal of the segment
+        bool ok = true;
+        auto qk = [&](int i) {
+          const int st = i % S, w = i & 1;
+          if (!mbar_wait(smem_u32(&full[st]), (uint32_t)(i / S) & 1u, quit)) { ok = false; return; }
+          tc_fence_after();
+          const uint32_t qb = q_base + (uint32_t)(so & 1) * C::kQ, kb = base + st * C::kTile;
+#pragma unroll
+          for (int ks = 0; ks < HD / 16; ++ks)
+            umma_bf16(tmem + w * 256, smem_desc_sw128(qb + (ks >> 2) * C::kQSub + (ks & 3) * 32), smem_desc_sw128(kb + (ks >> 2) * C::kSub + (ks & 3) * 32),
+                      id_s, ks > 0);
+          umma_commit(smem_u32(&s_ready[w]));
+          const int moved = i + 1 < n_mine ? move_on<kKeys>(a, at, 1) : 1;
+          if (moved) { umma_commit(smem_u32(&q_free[so & 1])); ++so; }
+        };
+        qk(0);
+        if (ok && n_mine > 1) qk(1);
+        for (int i = 0; i < n_mine && ok; ++i) {
+          const int st = i % S, w = i & 1;
+          if (!mbar_wait(smem_u32(&p_ready[w]), (uint32_t)(i >> 1) & 1u, quit)) break;
+          tc_fence_after();
+          const uint32_t vb = base + st * C::kTile + C::kHalf;
+#pragma unroll
+          for (int part = 2; part >= 0; --part)
+#pragma unroll
+            for (int ks = 0; ks < kKeys / 16; ++ks)
+              umma_bf16_ts(tmem + w * 256 + 128, tmem + w * 256 + part * 32 + ks * 8, desc_v(vb + ks * 2048), id_o, part < 2 || ks > 0);
+          umma_commit(smem_u32(&o_ready[w]));
+          umma_commit(smem_u32(&empty[st]));
+          if (i + 2 < n_mine) qk(i + 2);
+        }
+        // everything issued has completed, and its arrivals are made, before shared and tensor memory are given up
+        umma_commit(smem_u32(&drained));
+        const unsigned long long t0 = clock64();
+        while (!mbar_try(smem_u32(&drained), 0))
+          if ((unsigned long long)(clock64() - t0) > kSpinBudget) { *quit = 1; break; }
+      }
+      __syncwarp();
+    } else {
+      // ------------------------------------------------------------------------------------------ loads
+      const int lw = warp - 9;
+      Place ld = seg;
+      int so = 0, pending = -1;
+      bool ok = true;
+      auto landed = [&]() {                              // the copies of `pending` are here: for the tensor core to read
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&full[pending]));
+      };
+      if (lw < n_mine) so += move_on<kKeys>(a, ld, lw);
+      for (int i = lw; i < n_mine; i += kLoaders) {
+        const int st = i % S;
+        // ---- pages of the lanes' keys (lane, lane + 32)
+        const int see_from = window_first(ld.len + ld.qg * kQueries / group, a.window);
+        const int see_to = min(ld.len + min(nq - 1, ld.qg * kQueries + kQueries - 1) / group, a.cap - 1);
+        long long off[2];
+        unsigned int bad[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int t = tile_key(ld.k, ld.t, kKeys) + x * 32 + lane;
+          const bool seen = t <= see_to && (t >= see_from || t < a.n_sink);
+          off[x] = -1;
+          bool missing = false;
+          if (seen) {
+            const int e = t / a.pool.page_size, page = a.table[(long long)ld.b * a.width + e];
+            missing = page < 0 || page >= a.pool.n_pages;
+            if (!missing) off[x] = (long long)page * a.pool.page_stride + (long long)(t - e * a.pool.page_size) * a.pool.slot_stride;
+          }
+          bad[x] = __ballot_sync(0xffffffffu, missing);
+        }
+        if (i >= S && !__all_sync(0xffffffffu, mbar_try(smem_u32(&empty[st]), (uint32_t)(i / S - 1) & 1u))) {
+          if (pending >= 0) {                            // what waits for these copies may be what frees the stage
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            landed();
+            pending = -1;
+          }
+          if (!mbar_wait_warp(smem_u32(&empty[st]), (uint32_t)(i / S - 1) & 1u, quit)) { ok = false; break; }
+        }
+        if (ld.t == 0 || i == 0) {
+          // ---- the unit's queries, behind the products of the segment that had this buffer before
+          if (so >= 2 && !__all_sync(0xffffffffu, mbar_try(smem_u32(&q_free[so & 1]), (uint32_t)((so >> 1) - 1) & 1u))) {
+            if (pending >= 0) {
+              asm volatile("cp.async.wait_group 0;" ::: "memory");
+              landed();
+              pending = -1;
+            }
+            if (!mbar_wait_warp(smem_u32(&q_free[so & 1]), (uint32_t)((so >> 1) - 1) & 1u, quit)) { ok = false; break; }
+          }
+          const uint32_t qb = q_base + (uint32_t)(so & 1) * C::kQ;
+          for (int e = lane; e < kQueries * PER; e += 32) {
+            const int r = e / PER, q = min(ld.qg * kQueries + r, nq - 1), j = q / group, h = ld.kvh * group + q - j * group;
+            copy16(qb + uoff(kQueries, r, e % PER), (const __nv_bfloat16 *)a.q + ((long long)ld.b * a.c + j) * a.q_stride + h * HD + (e % PER) * 8, 16u);
+          }
+        }
+        if (lane == 0) { bad_keys[st][0] = bad[0]; bad_keys[st][1] = bad[1]; }
+        const __nv_bfloat16 *k0 = (const __nv_bfloat16 *)a.pool.k + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
+        const __nv_bfloat16 *v0 = (const __nv_bfloat16 *)a.pool.v + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
+        const uint32_t kb = base + st * C::kTile;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll 4
+          for (int y = 0; y < PER; ++y) {
+            const int r = y * (32 / PER) + lane / PER;
+            const long long o = __shfl_sync(0xffffffffu, off[x], r);
+            const uint32_t d = kb + uoff(kKeys, x * 32 + r, lane % PER), bytes = o < 0 ? 0u : 16u;      // keys that no row sees become zeros
+            copy16(d, k0 + (o < 0 ? 0 : o), bytes);
+            copy16(d + C::kHalf, v0 + (o < 0 ? 0 : o), bytes);
+          }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (pending >= 0) {
+          asm volatile("cp.async.wait_group 1;" ::: "memory");
+          landed();
+        }
+        pending = st;
+        if (i + kLoaders < n_mine) so += move_on<kKeys>(a, ld, kLoaders);
+      }
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      if (ok && pending >= 0) landed();
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    // -------------------------------------------------------------------------------------------- softmax
+    const int w = warp >> 2, row = tid & 127;
+    const uint32_t sc = tmem + w * 256 + ((uint32_t)(warp & 3) << 21), pr = sc + 128;           // this warp's 32 lanes
+    int i = w, done = 0, exchanges = 0;
+    uint32_t odd_phase = 0;
+    bool ok = true;
+    while (ok) {
+      const int seg_n = min(n_mine - done, seg.k.n - seg.t);
+      const int q0 = seg.qg * kQueries, q = q0 + row, qc = min(q, nq - 1), j = qc / group, h = seg.kvh * group + qc - j * group;
+      const int pos = seg.len + j, low = window_first(pos, a.window);
+      const int p_first = seg.len + q0 / group, p_last = seg.len + min(nq - 1, q0 + kQueries - 1) / group;
+      const int low_last = window_first(p_last, a.window);
+      float m = -INFINITY, l = 0.f, o[HD];
+#pragma unroll
+      for (int c = 0; c < HD; ++c) o[c] = 0.f;
+      for (; i < done + seg_n; i += 2) {
+        const int st = i % S;
+        const uint32_t turn = (uint32_t)(i >> 1) & 1u;
+        const int key0 = tile_key(seg.k, seg.t + i - done, kKeys);
+        // the scores; the tile's own barrier, long past, for what the loads wrote beside it
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[w]), turn, quit) && mbar_wait(smem_u32(&full[st]), (uint32_t)(i / S) & 1u, quit));
+        if (!ok) break;
+        tc_fence_after();
+        float s[kKeys];
+        tmem_ld32(sc, s);
+        tmem_ld32(sc + 32, s + 32);
+        const bool masked = key0 + kKeys - 1 > p_first || (key0 < low_last && key0 + kKeys > a.n_sink);
+        const unsigned int bad0 = bad_keys[st][0], bad1 = bad_keys[st][1];
+        if (masked || (bad0 | bad1)) {
+#pragma unroll
+          for (int k = 0; k < kKeys; ++k) {
+            const int t = key0 + k;
+            if ((k < 32 ? bad0 >> k : bad1 >> (k - 32)) & 1u) s[k] = quiet_nan();
+            if (t > pos || (t < low && t >= a.n_sink)) s[k] = -INFINITY;
+          }
+        }
+        float mx[4] = {m, s[1], s[2], s[3]};
+        mx[0] = fmaxf(mx[0], s[0]);
+#pragma unroll
+        for (int k = 4; k < kKeys; ++k) mx[k & 3] = fmaxf(mx[k & 3], s[k]);
+        mx[0] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        float corr = mx[0] == m ? 1.f : ex2((m - mx[0]) * sl2);                                // first tile: 2^-inf = 0
+        m = mx[0];
+        const float mb = m == -INFINITY ? 0.f : m * sl2;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kKeys; ++k) {
+          s[k] = ex2(fmaf(s[k], sl2, -mb));
+          sum[k & 3] += s[k];
+        }
+        l = fmaf(l, corr, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+        // values that are not finite, in a tile that some rows see more of than others: those keys are added row by row and
+        // taken out of the tile (a probability of zero would carry them to rows that do not see them)
+        if (masked && p_first != p_last) {
+          const uint32_t vb = base + st * C::kTile + C::kHalf;
+          unsigned char *vg = base_g + (vb - base);
+          unsigned int odd0 = 0, odd1 = 0;
+          for (int e = row; e < kKeys * PER; e += 128) {
+            const int r = e / PER;
+            const uint4 x = *reinterpret_cast<const uint4 *>(vg + uoff(kKeys, r, e % PER));
+            const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+            bool found = false;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) found |= (y[c] & 0x7f80u) == 0x7f80u || (y[c] & 0x7f800000u) == 0x7f800000u;
+            if (found) { if (r < 32) odd0 |= 1u << r; else odd1 |= 1u << (r - 32); }
+          }
+          if (odd0) atomicOr(&odd_keys[w][0], odd0);
+          if (odd1) atomicOr(&odd_keys[w][1], odd1);
+          mbar_arrive(smem_u32(&odd_bar[w]));
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&odd_bar[w]), odd_phase, quit));
+          if (!ok) break;
+          odd_phase ^= 1u;
+          odd0 = *(volatile unsigned int *)&odd_keys[w][0];
+          odd1 = *(volatile unsigned int *)&odd_keys[w][1];
+          if (odd0 | odd1) {
+#pragma unroll
+            for (int c = 0; c < HD; ++c) o[c] *= corr;
+            corr = 1.f;
+            for (unsigned long long left = ((unsigned long long)odd1 << 32) | odd0; left; left &= left - 1) {
+              const int kk = __ffsll((long long)left) - 1;
+              if (!sees(pos, key0 + kk, a.window, a.n_sink)) continue;
+              float p = 0.f;
+#pragma unroll
+              for (int k = 0; k < kKeys; ++k)
+                if (k == kk) p = s[k];
+#pragma unroll
+              for (int ch = 0; ch < PER; ++ch) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(vg + uoff(kKeys, kk, ch));
+                const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                  o[ch * 8 + 2 * c] = fmaf(p, low_half(y[c]), o[ch * 8 + 2 * c]);
+                  o[ch * 8 + 2 * c + 1] = fmaf(p, high_half(y[c]), o[ch * 8 + 2 * c + 1]);
+                }
+              }
+            }
+            mbar_arrive(smem_u32(&odd_bar[w]));
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&odd_bar[w]), odd_phase, quit));
+            if (!ok) break;
+            odd_phase ^= 1u;
+            for (int e = row; e < kKeys * PER; e += 128) {
+              const int r = e / PER;
+              if ((r < 32 ? odd0 >> r : odd1 >> (r - 32)) & 1u) *reinterpret_cast<uint4 *>(vg + uoff(kKeys, r, e % PER)) = make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async();
+            if (row == 0) odd_keys[w][0] = odd_keys[w][1] = 0u;
+          }
+        }
+        // ---- probabilities in three parts, cut off (8 bits each), over the scores
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int part = 0; part < 3; ++part) {
+            uint32_t r[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              float &p0 = s[half * 32 + 2 * k], &p1 = s[half * 32 + 2 * k + 1];
+              r[k] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+              if (part < 2) { p0 -= low_half(r[k]); p1 -= high_half(r[k]); }
+            }
+            tmem_st16(sc + part * 32 + half * 16, r);
+          }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before();
+        mbar_arrive(smem_u32(&p_ready[w]));
+        // ---- O = corr O + P.V
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&o_ready[w]), turn, quit));
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int c0 = 0; c0 < HD; c0 += 32) {
+          float y[32];
+          tmem_ld32(pr + c0, y);
+#pragma unroll
+          for (int c = 0; c < 32; ++c) o[c0 + c] = fmaf(o[c0 + c], corr, y[c]);
+        }
+        tc_fence_before();
+      }
+      if (!ok) break;
+      // ---- the groups' results: the second hands over, the first adds up and writes
+      const bool whole = seg_n == seg.k.n;
+      float *part = a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * (kQueries * (HD + 2));
+      float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + row * HD;
+#pragma unroll
+      for (int c0 = 0; c0 < HD; c0 += 64, ++exchanges) {
+        if (w == 1) {
+          if (exchanges > 0) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ex_free), (uint32_t)(exchanges - 1) & 1u, quit));
+          if (!ok) break;
+          if (c0 == 0) ml[row] = make_float2(m, l);
+#pragma unroll
+          for (int c = 0; c < 16; ++c) exchange[row * 16 + (c ^ (row & 15))] = make_float4(o[c0 + 4 * c], o[c0 + 4 * c + 1], o[c0 + 4 * c + 2], o[c0 + 4 * c + 3]);
+          mbar_arrive(smem_u32(&ex_full));
+        } else {
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ex_full), (uint32_t)exchanges & 1u, quit));
+          if (!ok) break;
+          const float2 other = ml[row];
+          const float M = fmaxf(m, other.x), f0 = part_weight(make_float2(m, l), M, sl2), f1 = part_weight(other, M, sl2);
+          const float den = fmaf(l, f0, other.y * f1), f = whole ? result_scale(a, pos, den) : 1.f;
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            const float4 x = exchange[row * 16 + (c ^ (row & 15))];
+            const float4 y = make_float4(fmaf(f1, x.x, f0 * o[c0 + 4 * c]) * f, fmaf(f1, x.y, f0 * o[c0 + 4 * c + 1]) * f,
+                                         fmaf(f1, x.z, f0 * o[c0 + 4 * c + 2]) * f, fmaf(f1, x.w, f0 * o[c0 + 4 * c + 3]) * f);
+            if (q < nq) *reinterpret_cast<float4 *>(to + c0 + 4 * c) = y;
+          }
+          if (!whole && c0 == 0 && q < nq) *reinterpret_cast<float2 *>(part + kQueries * HD + row * 2) = make_float2(M, den);
+          mbar_arrive(smem_u32(&ex_free));
+        }
+      }
+      done += seg_n;
+      if (done == n_mine) break;
+      move_on<kKeys>(a, seg, seg_n);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) tmem_dealloc(tmem, 512);
+  if (tid == 0) a.status[blockIdx.x] = gave_up != 0;
+}
+
+template <int HD>
+cudaError_t launch(const PagedAttnArgs &a, cudaStream_t st) {
+  using C = UmmaCfg<HD>;
+  static bool done[kMaxDevices] = {false};
+  const int dev = current_device_slot();
+  if (!done[dev]) {
+    // the register split is only there to be had if the launch holds what it adds up to
+    cudaFuncAttributes at;
+    if (cudaError_t e = cudaFuncGetAttributes(&at, paged_umma_kernel<HD>)) return e;
+    if (at.numRegs * kThreads < 256 * kSoftRegs + 128 * kLoadRegs) return cudaErrorInvalidConfiguration;
+    if (cudaError_t e = allow_smem(paged_umma_kernel<HD>, C::kSmem, done)) return e;
+  }
+  paged_umma_kernel<HD><<<kWorkers, kThreads, C::kSmem, st>>>(a);
+  if (cudaError_t e = cudaGetLastError()) return e;
+  return launch_combine<HD, kQueries, kKeys>(a, kWorkers, st);
+}
+
+size_t status_bytes() { return (kWorkers * sizeof(unsigned int) + 255) / 256 * 256; }
+
+}  // namespace
+
+size_t paged_umma_scratch(int hd) { return status_bytes() + (size_t)kWorkers * 2 * kQueries * (hd + 2) * sizeof(float); }
+
+cudaError_t launch_paged_umma(PagedAttnArgs a, int hd, cudaStream_t st) {
+  a.groups = (a.hq / a.pool.n_kv_heads * a.c + kQueries - 1) / kQueries;
+  a.status = (unsigned int *)a.parts;
+  a.parts = (float *)((char *)a.parts + status_bytes());
+  return hd == 128 ? launch<128>(a, st) : launch<64>(a, st);
+}
+
+}  // namespace fc
