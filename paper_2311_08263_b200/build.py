@@ -9,7 +9,7 @@ CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libfastcot.so")
 SOURCES = ["fc_api.cu", "k_simt.cu", "k_umma.cu", "k_attn.cu", "k_attn_stream.cu", "k_attn_short.cu", "k_bulk.cu", "k_cluster.cu", "k_small.cu", "k_paged.cu",
-           "k_paged_attn.cu", "k_paged_umma.cu", "k_pages.cu", "fc_noalloc.cu"]
+           "k_paged_attn.cu", "k_paged_umma.cu", "k_paged_fma.cu", "k_pages.cu", "fc_noalloc.cu"]
 
 
 def _stale() -> bool:

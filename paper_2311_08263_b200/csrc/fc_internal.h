@@ -376,6 +376,8 @@ struct PagedAttnArgs;
 size_t paged_attn_scratch(int nq, int hd, int dtype);       // nq: queries of a kv head
 size_t paged_umma_scratch(int hd);
 cudaError_t launch_paged_umma(PagedAttnArgs a, int hd, cudaStream_t st);
-cudaError_t launch_paged_attn(const PagedAttnArgs &a, int dtype, int hd, cudaStream_t st);
+size_t paged_fma_scratch(int hd);
+cudaError_t launch_paged_fma(const PagedAttnArgs &a, int hd, cudaStream_t st);
+cudaError_t launch_paged_attn(PagedAttnArgs a, int dtype, int hd, cudaStream_t st);
 
 }  // namespace fc

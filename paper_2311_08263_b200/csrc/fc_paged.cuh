@@ -115,6 +115,144 @@ __device__ __forceinline__ float result_scale(const PagedAttnArgs &a, int pos, f
   return pos >= a.cap ? quiet_nan() : den == 0.f ? 0.f : 1.0f / den;
 }
 
+// Byte offset of 16-byte piece `ch` of key `r` in a tile of KEYS rows of ROW bytes: sub-tiles of 128 bytes a row, pieces permuted so that eight rows at
+// one piece lie in different banks.
+template <int KEYS, int ROW>
+__device__ __forceinline__ uint32_t poff(int r, int ch) {
+  if (ROW == 64) return (uint32_t)r * 64u + (uint32_t)((ch ^ ((r >> 1) & 3)) << 4);
+  return (uint32_t)(ch >> 3) * (KEYS * 128u) + (uint32_t)r * 128u + (uint32_t)(((ch & 7) ^ (r & 7)) << 4);
+}
+
+// A warp's own stream of tiles: every STEP-th tile of a CTA's piece of work into a ring of S stages (keys, then values, of KEYS rows of ROW bytes).
+// The lanes' keys are looked up in the table a tile ahead of the copies, which first use what was read then.
+template <int KEYS, int ROW, int S, int STEP, int QUERIES, bool LINE>
+struct TileStream {
+  static constexpr uint32_t kHalf = KEYS * ROW, kTile = 2 * kHalf;
+  static constexpr int PER = ROW / 16, RPI = 32 / PER;   // 16-byte pieces of a row; rows that the lanes load at once
+  static constexpr int kUnseen = -2;                     // a key that no query sees; -1: the table has no page for it
+  static_assert(KEYS <= 32 && 32 % KEYS == 0 && KEYS % RPI == 0, "lanes, keys and rows");
+  const PagedAttnArgs &a;
+  Place at;
+  int i, n, nq, group;                                   // next tile, tiles of the piece; queries of a kv head, heads of the group
+  int see_from, see_to;                                  // keys that some query of the unit sees: the sinks, and from .. to
+  int page, slot;
+  uint32_t ring;                                         // shared memory
+  unsigned int *bad_keys;                                // [S] keys of a tile whose page is missing
+
+  __device__ __forceinline__ TileStream(const PagedAttnArgs &args, const Place &begin, int first, int count, uint32_t smem, unsigned int *bad)
+      : a(args), at(begin), i(first), n(count), page(kUnseen), slot(0), ring(smem), bad_keys(bad) {
+    group = a.hq / a.pool.n_kv_heads;
+    nq = group * a.c;
+    if (i < n) {
+      if (LINE) move_on<KEYS>(a, at, first);
+      else at.t += first;
+      unit_keys();
+      look_up();
+    }
+  }
+  __device__ __forceinline__ void unit_keys() {
+    see_from = window_first(at.len + at.qg * QUERIES / group, a.window);                 // the first row's window reaches furthest back
+    see_to = min(at.len + min(nq - 1, at.qg * QUERIES + QUERIES - 1) / group, a.cap - 1);
+  }
+  __device__ __forceinline__ void look_up() {
+    const int t = tile_key(at.k, at.t, KEYS) + (threadIdx.x & (KEYS - 1));
+    page = kUnseen;
+    if (t <= see_to && (t >= see_from || t < a.n_sink)) {
+      const int e = t / a.pool.page_size;
+      slot = t - e * a.pool.page_size;
+      page = max(-1, a.table[(long long)at.b * a.width + e]);
+    }
+  }
+  // Copies of the next tile (or of nothing) into a stage, as one group.
+  __device__ __forceinline__ void request(int stage) {
+    if (i < n) {
+      const int lane = threadIdx.x & 31;
+      const bool there = page >= 0 && page < a.pool.n_pages;
+      const unsigned int bad = __ballot_sync(0xffffffffu, !there && page != kUnseen);
+      if (lane == 0) bad_keys[stage] = bad;              // (KEYS < 32: the lanes hold the keys several times)
+      const long long off = there ? (long long)page * a.page_bytes + (long long)slot * a.slot_bytes : -1;
+      const uint32_t kb = ring + stage * kTile;
+      const char *k0 = (const char *)a.pool.k + at.kvh * a.head_bytes + (lane % PER) * 16;
+      const char *v0 = (const char *)a.pool.v + at.kvh * a.head_bytes + (lane % PER) * 16;
+#pragma unroll
+      for (int y = 0; y < KEYS / RPI; ++y) {
+        const int r = y * RPI + lane / PER;
+        const long long o = __shfl_sync(0xffffffffu, off, r);
+        const uint32_t d = kb + poff<KEYS, ROW>(r, lane % PER), bytes = o < 0 ? 0u : 16u;      // keys that no row sees become zeros
+        copy16(d, k0 + (o < 0 ? 0 : o), bytes);
+        copy16(d + kHalf, v0 + (o < 0 ? 0 : o), bytes);
+      }
+      i += STEP;
+      if (i < n) {
+        if (LINE) {
+          if (move_on<KEYS>(a, at, STEP)) unit_keys();
+        } else {
+          at.t += STEP;
+        }
+        look_up();
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+};
+
+// What a CTA has to do: the place of its first tile, and how many there are.  LINE: its piece of the line; else its share of one unit (grid: CTAs of the
+// cluster, units, sequences).  False where the line has nothing for it.
+template <int KEYS, bool LINE>
+__device__ __forceinline__ bool my_piece(const PagedAttnArgs &a, Place &seg, int &n) {
+  if (LINE) {
+    long long total, unused;
+    count_tiles<KEYS>(a, 0, total, unused);
+    const long long chunk = chunk_of(total, gridDim.x), f0 = chunk * blockIdx.x;
+    if (f0 >= total) return false;
+    n = (int)(total - f0 < chunk ? total - f0 : chunk);
+    seg = find_place<KEYS>(a, f0);
+  } else {
+    seg.b = blockIdx.z; seg.kvh = blockIdx.y / a.groups; seg.qg = blockIdx.y - seg.kvh * a.groups;
+    seg.k = seq_tiles<KEYS>(a, seg.b, seg.len);
+    const int cut = (seg.k.n + gridDim.x - 1) / gridDim.x;
+    seg.t = cut * blockIdx.x;
+    n = max(0, min(cut, seg.k.n - seg.t));
+  }
+  return true;
+}
+
+// The parts of a cluster: un-normalised sums [rows][HD] at `sums` and (max, sum) at `ml` in each CTA's shared memory.  Every CTA writes a share of the rows.
+template <int HD>
+__device__ __forceinline__ void join_cluster(const PagedAttnArgs &a, const Place &seg, int q0, int rows, uint32_t sums, uint32_t ml, int threads) {
+  const int ns = gridDim.x, group = a.hq / a.pool.n_kv_heads;
+  const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
+  cluster_sync_all();
+  for (int e = blockIdx.x * threads + threadIdx.x; e < rows * (HD / 4); e += ns * threads) {
+    const int row = e / (HD / 4), c4 = e - row * (HD / 4);
+    float2 mv[8];
+    float4 ov[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      mv[r] = make_float2(-INFINITY, 0.f);
+      ov[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < ns) {
+        mv[r] = ld_cluster_f2(map_to_cta(ml + (uint32_t)row * 8u, (uint32_t)r));
+        ov[r] = ld_cluster_f4(map_to_cta(sums + (uint32_t)(row * HD + c4 * 4) * 4u, (uint32_t)r));
+      }
+    }
+    float M = -INFINITY, den = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) M = fmaxf(M, mv[r].x);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float f = part_weight(mv[r], M, sl2);
+      den = fmaf(mv[r].y, f, den);
+      acc.x = fmaf(f, ov[r].x, acc.x); acc.y = fmaf(f, ov[r].y, acc.y); acc.z = fmaf(f, ov[r].z, acc.z); acc.w = fmaf(f, ov[r].w, acc.w);
+    }
+    const int q = q0 + row, j = q / group, h = seg.kvh * group + q - j * group;
+    const float f = seg.len < 0 ? 0.f : result_scale(a, seg.len + j, den);
+    *reinterpret_cast<float4 *>(a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD + c4 * 4) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+  }
+  cluster_sync_all();                                    // the others may still be reading this CTA's memory
+}
+
 // ------------------------------------------------------------------------------------ joining the parts of a unit
 // A block takes block_rows queries of a unit: with items = queries x hd / 4 pieces of four elements, threads are groups that take turns at the
 // parts.  A few units have many parts each (one sequence, four kv heads: 37), and then a query per block reads them all at once.
@@ -170,7 +308,7 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
           v[i] = make_float2(-INFINITY, 0.f);
           x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (at <= w.last) {
-            const float *part = a.parts + ((long long)at * 2 + part_place(begin, at, chunk)) * (Q * (HD + 2));
+            const float *part = a.parts + ((long long)at * 2 + part_place(begin, at, chunk)) * part_floats(Q, HD);
             v[i] = __ldcg(reinterpret_cast<const float2 *>(part + Q * HD + (row0 + row) * 2));
             x[i] = __ldcg(reinterpret_cast<const float4 *>(part + (row0 + row) * HD + c4 * 4));
           }
@@ -237,6 +375,29 @@ cudaError_t allow_smem(K kernel, size_t bytes, bool *done) {
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   done[dev] = e == cudaSuccess;
   return e;
+}
+
+// The line and the kernel that joins its parts, or clusters where paged_cluster says so.
+template <int HD, int Q, int KEYS, typename L, typename C>
+cudaError_t launch_units(PagedAttnArgs a, L line, C cluster, int warps, size_t smem, bool *line_done, bool *cluster_done, cudaStream_t st) {
+  const int nq = a.hq / a.pool.n_kv_heads * a.c;
+  a.groups = (nq + Q - 1) / Q;
+  const int ctas = paged_cluster(a.batch, a.groups * a.pool.n_kv_heads, a.cap, a.c, a.window, a.n_sink, KEYS, warps, kWorkers);
+  if (ctas == 0) {
+    if (cudaError_t e = allow_smem(line, smem, line_done)) return e;
+    line<<<kWorkers, warps * 32, smem, st>>>(a);
+    if (cudaError_t e = cudaGetLastError()) return e;
+    return launch_combine<HD, Q, KEYS>(a, kWorkers, st);
+  }
+  if (cudaError_t e = allow_smem(cluster, smem, cluster_done)) return e;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = dim3(ctas, a.groups * a.pool.n_kv_heads, a.batch); cfg.blockDim = dim3(warps * 32); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, cluster, a);
 }
 
 }  // namespace

@@ -25,7 +25,9 @@ struct PagedAttnArgs {
   const void *q; long long q_stride;      // elements
   float *out;             // [batch * c, hq * hd]
   int batch, c, hq, window, n_sink;       // n_sink is 0 without a window
-  int groups;             // groups of queries of a kv head (set by the launcher)
+  // set by the launcher: groups of queries of a kv head, the pool's strides in bytes
+  int groups;
+  long long page_bytes, head_bytes, slot_bytes;
   float *parts;           // scratch: two parts per worker, [queries][hd] sums and [queries] (max, sum)
   unsigned int *status;   // scratch of the kernel that has waits, else null: per worker, 1 where a wait ran out
 };
@@ -74,6 +76,8 @@ FC_HD int tile_key(const KeyTiles &t, int i, int keys) { return (i < t.sinks ? i
 // All tiles of a call stand in one line: sequence by sequence, unit (kv head, group of queries) by unit, and each of `workers` takes
 // `chunk` of them in a row.  The parts of the unit at [begin, begin + n) and where worker i left its part: place 0 for what a
 // worker begins with, 1 for what it ends with.
+// A part: [queries][hd] sums, then [queries] (max, sum), in whole 16-byte pieces (sums are written and read four at a time).
+FC_HD constexpr int part_floats(int queries, int hd) { return queries * hd + (2 * queries + 3) / 4 * 4; }
 struct UnitParts { int first, last; };
 FC_HD long long chunk_of(long long total, int workers) { return (total + workers - 1) / workers; }
 FC_HD UnitParts unit_parts(long long begin, int n, long long chunk) { return {(int)(begin / chunk), (int)((begin + n - 1) / chunk)}; }

@@ -25,7 +25,8 @@ constexpr int kWarps = 8, kThreads = kWarps * 32;
 
 template <int HD>
 struct PagedCfg {
-  static constexpr uint32_t kHalf = kKeys * HD * 2, kTile = 2 * kHalf;
+  static constexpr int kRow = HD * 2;                              // bytes of a key
+  static constexpr uint32_t kHalf = kKeys * kRow, kTile = 2 * kHalf;
   static constexpr int S = HD == 128 ? 3 : 6;                      // stages of a warp's ring
   static constexpr int DB = HD / 16;                               // blocks of 16 elements of the output
   static constexpr uint32_t kRing = kWarps * S * kTile;
@@ -33,13 +34,6 @@ struct PagedCfg {
   static constexpr size_t kSmem = 128 + kRing + kExchange;
 };
 
-// Byte offset of 16-byte piece `ch` of key `r` in a tile: rows of 128 bytes (hd 128: two sub-tiles), pieces permuted so that eight
-// rows at one piece lie in different banks.
-template <int HD>
-__device__ __forceinline__ uint32_t poff(int r, int ch) {
-  if (HD == 32) return (uint32_t)r * 64u + (uint32_t)((ch ^ ((r >> 1) & 3)) << 4);
-  return (uint32_t)(ch >> 3) * (kKeys * 128u) + (uint32_t)r * 128u + (uint32_t)(((ch & 7) ^ (r & 7)) << 4);
-}
 // 8 x 8 transpose of 16-bit elements across a warp
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
@@ -51,7 +45,7 @@ template <int HD, int QN, bool LINE>
 __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_constant__ PagedAttnArgs a) {
   using C = PagedCfg<HD>;
   constexpr int W = kWarps, S = C::S, KS = HD / 16, DB = C::DB, Q = 8 * QN;
-  constexpr int PER = HD / 8, RPI = 32 / PER;            // 16-byte pieces of a row; rows that the lanes of a warp load at once
+  constexpr int PER = HD / 8;                            // 16-byte pieces of a row
   constexpr int OWN = (DB + W - 1) / W;                  // blocks of elements that a warp adds up
   if (LINE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
@@ -69,76 +63,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
   Place seg;                                             // where the segment (a unit's tiles in this CTA's piece) begins
   int n_mine;
-  if (LINE) {
-    long long total, unused;
-    count_tiles<kKeys>(a, 0, total, unused);
-    const long long chunk = chunk_of(total, gridDim.x), f0 = chunk * blockIdx.x;
-    if (f0 >= total) return;
-    n_mine = (int)(total - f0 < chunk ? total - f0 : chunk);
-    seg = find_place<kKeys>(a, f0);
-  } else {
-    seg.b = blockIdx.z; seg.kvh = blockIdx.y / a.groups; seg.qg = blockIdx.y - seg.kvh * a.groups;
-    seg.k = seq_tiles<kKeys>(a, seg.b, seg.len);
-    const int cut = (seg.k.n + gridDim.x - 1) / gridDim.x;
-    seg.t = cut * blockIdx.x;
-    n_mine = max(0, min(cut, seg.k.n - seg.t));
-  }
-
-  // ---- what is requested next: a tile of 16 keys, the lanes' keys (twice) looked up a tile ahead of the copies
-  Place ld = seg;
-  int ld_i = warp, see_from = 0, see_to = -1;            // keys that some query of the unit sees: the sinks, and from .. to
-  constexpr int kUnseen = -2;                            // a key that no query sees; -1: the table has no page for it
-  int next_page = kUnseen, next_slot = 0;                // page and slot of the lane's key: used a tile later, when they have arrived
-  auto unit_keys = [&]() {
-    see_from = window_first(ld.len + ld.qg * Q / group, a.window);                       // the first row's window reaches furthest back
-    see_to = min(ld.len + min(nq - 1, ld.qg * Q + Q - 1) / group, a.cap - 1);
-  };
-  auto look_up = [&]() {
-    const int t = tile_key(ld.k, ld.t, kKeys) + (lane & 15);
-    next_page = kUnseen;
-    if (t <= see_to && (t >= see_from || t < a.n_sink)) {
-      const int i = t / a.pool.page_size;
-      next_slot = t - i * a.pool.page_size;
-      next_page = max(-1, a.table[(long long)ld.b * a.width + i]);
-    }
-  };
-  auto request = [&](int stage) {
-    if (ld_i < n_mine) {
-      const bool there = next_page >= 0 && next_page < a.pool.n_pages;
-      const long long off = there ? (long long)next_page * a.pool.page_stride + (long long)next_slot * a.pool.slot_stride : -1;
-      const unsigned int bad = __ballot_sync(0xffffffffu, !there && next_page != kUnseen) & 0xffffu;
-      if (lane == 0) bad_keys[warp][stage] = bad;
-      const uint32_t kb = ring + stage * C::kTile;
-      const __nv_bfloat16 *k0 = (const __nv_bfloat16 *)a.pool.k + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
-      const __nv_bfloat16 *v0 = (const __nv_bfloat16 *)a.pool.v + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
+  if (!my_piece<kKeys, LINE>(a, seg, n_mine)) return;
+  TileStream<kKeys, C::kRow, S, W, Q, LINE> stream(a, seg, warp, n_mine, ring, bad_keys[warp]);
 #pragma unroll
-      for (int i = 0; i < kKeys / RPI; ++i) {
-        const int r = i * RPI + lane / PER;
-        const long long o = __shfl_sync(0xffffffffu, off, r);
-        const uint32_t d = kb + poff<HD>(r, lane % PER), bytes = o < 0 ? 0u : 16u;      // keys that no row sees become zeros
-        copy16(d, k0 + (o < 0 ? 0 : o), bytes);
-        copy16(d + C::kHalf, v0 + (o < 0 ? 0 : o), bytes);
-      }
-      ld_i += W;
-      if (ld_i < n_mine) {
-        if (LINE) {
-          if (move_on<kKeys>(a, ld, W)) unit_keys();
-        } else {
-          ld.t += W;
-        }
-        look_up();
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  if (ld_i < n_mine) {
-    if (LINE) move_on<kKeys>(a, ld, warp);
-    else ld.t += warp;
-    unit_keys();
-    look_up();
-  }
-#pragma unroll
-  for (int s = 0; s < S - 1; ++s) request(s);
+  for (int s = 0; s < S - 1; ++s) stream.request(s);
 
   int stage = 0;
   int i = warp;                                          // this warp's next tile in the piece
@@ -181,7 +109,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
     for (; i < done + seg_n; i += W) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
       __syncwarp();                                      // everybody's copies are here, and the stage before is free
-      request(stage == 0 ? S - 1 : stage - 1);
+      stream.request(stage == 0 ? S - 1 : stage - 1);
       const int key0 = tile_key(seg.k, seg.t + i - done, kKeys);
       const uint32_t kb = ring + stage * C::kTile, vb = kb + C::kHalf;
       const unsigned int bad = bad_keys[warp][stage];
@@ -194,8 +122,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
 #pragma unroll
       for (int ks = 0; ks < KS; ks += 2) {
         uint32_t k0[4], k1[4];
-        ldsm4(kb + poff<HD>(lane & 15, ks * 2 + (lane >> 4)), k0);
-        ldsm4(kb + poff<HD>(lane & 15, ks * 2 + 2 + (lane >> 4)), k1);
+        ldsm4(kb + poff<kKeys, C::kRow>(lane & 15, ks * 2 + (lane >> 4)), k0);
+        ldsm4(kb + poff<kKeys, C::kRow>(lane & 15, ks * 2 + 2 + (lane >> 4)), k1);
 #pragma unroll
         for (int n = 0; n < QN; ++n) mma16816(s[n], k0, qf[n][ks][0], qf[n][ks][1]);
 #pragma unroll
@@ -240,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
         unsigned char *vg = base_g + (vb - base);
         unsigned int odd = 0;
         for (int e = lane; e < kKeys * PER; e += 32) {
-          const uint4 x = *reinterpret_cast<const uint4 *>(vg + poff<HD>(e / PER, e % PER));
+          const uint4 x = *reinterpret_cast<const uint4 *>(vg + poff<kKeys, C::kRow>(e / PER, e % PER));
           const uint32_t y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
           for (int w = 0; w < 4; ++w)
@@ -268,14 +196,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
                   for (int e = 0; e < 2; ++e) {
-                    const __nv_bfloat16 y = *reinterpret_cast<const __nv_bfloat16 *>(vg + poff<HD>(kk, d * 2 + e) + g4 * 2);
+                    const __nv_bfloat16 y = *reinterpret_cast<const __nv_bfloat16 *>(vg + poff<kKeys, C::kRow>(kk, d * 2 + e) + g4 * 2);
                     o[n][d][2 * e + x] = fmaf(p, __bfloat162float(y), o[n][d][2 * e + x]);
                   }
               }
           }
           __syncwarp();
           for (int e = lane; e < kKeys * PER; e += 32)
-            if (odd >> (e / PER) & 1u) *reinterpret_cast<uint4 *>(vg + poff<HD>(e / PER, e % PER)) = make_uint4(0, 0, 0, 0);
+            if (odd >> (e / PER) & 1u) *reinterpret_cast<uint4 *>(vg + poff<kKeys, C::kRow>(e / PER, e % PER)) = make_uint4(0, 0, 0, 0);
           __syncwarp();
         }
       }
@@ -297,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
 #pragma unroll
       for (int d = 0; d < DB; ++d) {
         uint32_t vf[4];
-        ldsm4t(vb + poff<HD>((lane & 7) + ((lane >> 4) << 3), d * 2 + ((lane >> 3) & 1)), vf);
+        ldsm4t(vb + poff<kKeys, C::kRow>((lane & 7) + ((lane >> 4) << 3), d * 2 + ((lane >> 3) & 1)), vf);
         float y[QN][4];
 #pragma unroll
         for (int n = 0; n < QN; ++n)
@@ -327,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
       }
     const bool whole = LINE ? seg_n == seg.k.n : gridDim.x == 1;
     // where sums go that are not the whole unit's: scratch, or this CTA's shared memory (the ring, drained)
-    float *part = LINE ? a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * (Q * (HD + 2)) : reinterpret_cast<float *>(base_g);
+    float *part = LINE ? a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * part_floats(Q, HD) : reinterpret_cast<float *>(base_g);
     if (!LINE) {
       asm volatile("cp.async.wait_all;" ::: "memory");
       __syncthreads();
@@ -396,129 +324,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
     return;
   }
   if (gridDim.x == 1) return;
-  // ---- the cluster's parts: un-normalised sums and (max, sum) of each CTA in its shared memory
-  cluster_sync_all();
-  const int q0 = seg.qg * Q, rows = min(Q, nq - q0), ns = gridDim.x;
-  const uint32_t ml_addr = smem_u32(ml_cta);
-  for (int e = blockIdx.x * kThreads + tid; e < rows * (HD / 4); e += ns * kThreads) {
-    const int row = e / (HD / 4), c4 = e - row * (HD / 4);
-    float2 mv[8];
-    float4 ov[8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      mv[r] = make_float2(-INFINITY, 0.f);
-      ov[r] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < ns) {
-        mv[r] = ld_cluster_f2(map_to_cta(ml_addr + (uint32_t)row * 8u, (uint32_t)r));
-        ov[r] = ld_cluster_f4(map_to_cta(base + (uint32_t)(row * HD + c4 * 4) * 4u, (uint32_t)r));
-      }
-    }
-    float M = -INFINITY, den = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int r = 0; r < 8; ++r) M = fmaxf(M, mv[r].x);
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      const float f = part_weight(mv[r], M, sl2);
-      den = fmaf(mv[r].y, f, den);
-      acc.x = fmaf(f, ov[r].x, acc.x); acc.y = fmaf(f, ov[r].y, acc.y); acc.z = fmaf(f, ov[r].z, acc.z); acc.w = fmaf(f, ov[r].w, acc.w);
-    }
-    const int q = q0 + row, j = q / group, h = seg.kvh * group + q - j * group;
-    const float f = seg.len < 0 ? 0.f : result_scale(a, seg.len + j, den);
-    *reinterpret_cast<float4 *>(a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD + c4 * 4) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-  }
-  cluster_sync_all();                                    // the others may still be reading this CTA's memory
-}
-
-// ------------------------------------------------------------------------------------ fp32: a block per row and query head
-// The warps take turns at the keys, a lane holds HD / 32 elements.
-template <int HD>
-__global__ void __launch_bounds__(128) paged_fma_kernel(const __grid_constant__ PagedAttnArgs a) {
-  constexpr int E = HD / 32;
-  const int r = blockIdx.x, h = blockIdx.y, b = r / a.c, kvh = h / (a.hq / a.pool.n_kv_heads);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int len = clamp_len(a.kv_len[b], a.cap), p = len + (r - b * a.c);
-  __shared__ float part[4][HD + 2];
-  float q[E], o[E], m = -INFINITY, l = 0.f;
-  const float *qr = (const float *)a.q + r * a.q_stride + h * HD + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; ++e) { q[e] = qr[e] * rsqrtf((float)HD); o[e] = 0.f; }
-  const int32_t *row = a.table + (long long)b * a.width;
-  const int first = len < 0 ? 0 : window_first(p, a.window), sinks = len < 0 ? 0 : min(a.n_sink, first);
-  const int n = len < 0 ? 0 : sinks + p + 1 - first;
-  for (int i = warp; i < n; i += 4) {
-    const int t = i < sinks ? i : first + i - sinks;
-    const int page = page_of(row, a.width, t, a.pool.page_size, a.pool.n_pages);
-    const long long at = (long long)page * a.pool.page_stride + kvh * a.pool.head_stride + (t % a.pool.page_size) * a.pool.slot_stride + lane * E;
-    float s = 0.f, v[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      s = fmaf(q[e], page < 0 ? NAN : ((const float *)a.pool.k)[at + e], s);
-      v[e] = page < 0 ? NAN : ((const float *)a.pool.v)[at + e];
-    }
-#pragma unroll
-    for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);
-    const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : expf(m - mn), w = expf(s - mn);
-    l = l * f + w;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * f + w * v[e];
-    m = mn;
-  }
-#pragma unroll
-  for (int e = 0; e < E; ++e) part[warp][lane * E + e] = o[e];
-  if (lane == 0) { part[warp][HD] = m; part[warp][HD + 1] = l; }
-  __syncthreads();
-  for (int e = threadIdx.x; e < HD; e += 128) {
-    float M = -INFINITY, den = 0.f, sum = 0.f;
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, part[w][HD]);
-    for (int w = 0; w < 4; ++w) {
-      const float f = part[w][HD] == -INFINITY && part[w][HD + 1] == 0.f ? 0.f : expf(part[w][HD] - M);
-      den += f * part[w][HD + 1];
-      sum += f * part[w][e];
-    }
-    a.out[((long long)r * a.hq + h) * HD + e] = den == 0.f ? 0.f : sum / den;
-  }
+  const int q0 = seg.qg * Q;
+  join_cluster<HD>(a, seg, q0, min(Q, nq - q0), base, smem_u32(ml_cta), kThreads);
 }
 
 // ------------------------------------------------------------------------------------ host side
 template <int HD, int QN>
-cudaError_t launch_line(const PagedAttnArgs &a, cudaStream_t st) {
-  using C = PagedCfg<HD>;
-  static bool done[kMaxDevices] = {false};
-  if (cudaError_t e = allow_smem(paged_mma_kernel<HD, QN, true>, C::kSmem, done)) return e;
-  paged_mma_kernel<HD, QN, true><<<kWorkers, kThreads, C::kSmem, st>>>(a);
-  if (cudaError_t e = cudaGetLastError()) return e;
-  return launch_combine<HD, 8 * QN, kKeys>(a, kWorkers, st);
-}
-
-template <int HD, int QN>
-cudaError_t launch_cluster(const PagedAttnArgs &a, int ctas, cudaStream_t st) {
-  using C = PagedCfg<HD>;
-  static bool done[kMaxDevices] = {false};
-  if (cudaError_t e = allow_smem(paged_mma_kernel<HD, QN, false>, C::kSmem, done)) return e;
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof cfg);
-  cfg.gridDim = dim3(ctas, a.groups * a.pool.n_kv_heads, a.batch); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, paged_mma_kernel<HD, QN, false>, a);
-}
-
-template <int HD, int QN>
-cudaError_t launch_mma(PagedAttnArgs a, cudaStream_t st) {
-  const int nq = a.hq / a.pool.n_kv_heads * a.c;
-  a.groups = (nq + 8 * QN - 1) / (8 * QN);
-  const int ctas = paged_cluster(a.batch, a.groups * a.pool.n_kv_heads, a.cap, a.c, a.window, a.n_sink, kKeys, kWarps, kWorkers);
-  return ctas ? launch_cluster<HD, QN>(a, ctas, st) : launch_line<HD, QN>(a, st);
+cudaError_t launch_mma(const PagedAttnArgs &a, cudaStream_t st) {
+  static bool line[kMaxDevices] = {false}, cluster[kMaxDevices] = {false};
+  return launch_units<HD, 8 * QN, kKeys>(a, paged_mma_kernel<HD, QN, true>, paged_mma_kernel<HD, QN, false>, kWarps, PagedCfg<HD>::kSmem, line, cluster, st);
 }
 template <int HD>
-cudaError_t launch_hd(const PagedAttnArgs &a, int dtype, cudaStream_t st) {
-  if (dtype == FC_F32) {
-    paged_fma_kernel<HD><<<dim3(a.batch * a.c, a.hq), 128, 0, st>>>(a);
-    return cudaGetLastError();
-  }
+cudaError_t launch_hd(const PagedAttnArgs &a, cudaStream_t st) {
   const int nq = a.hq / a.pool.n_kv_heads * a.c;
   if (paged_umma(nq, HD)) return launch_paged_umma(a, HD, st);
   return nq <= 8 ? launch_mma<HD, 1>(a, st) : launch_mma<HD, 2>(a, st);
@@ -527,12 +344,15 @@ cudaError_t launch_hd(const PagedAttnArgs &a, int dtype, cudaStream_t st) {
 }  // namespace
 
 size_t paged_attn_scratch(int nq, int hd, int dtype) {
-  if (dtype == FC_F32) return 256;
-  return paged_umma(nq, hd) ? paged_umma_scratch(hd) : (size_t)kWorkers * 2 * 16 * (hd + 2) * sizeof(float);
+  if (dtype == FC_F32) return paged_fma_scratch(hd);
+  return paged_umma(nq, hd) ? paged_umma_scratch(hd) : (size_t)kWorkers * 2 * part_floats(16, hd) * sizeof(float);
 }
 
-cudaError_t launch_paged_attn(const PagedAttnArgs &a, int dtype, int hd, cudaStream_t st) {
-  return hd == 128 ? launch_hd<128>(a, dtype, st) : hd == 64 ? launch_hd<64>(a, dtype, st) : launch_hd<32>(a, dtype, st);
+cudaError_t launch_paged_attn(PagedAttnArgs a, int dtype, int hd, cudaStream_t st) {
+  const int es = dtype == FC_F32 ? 4 : 2;
+  a.page_bytes = a.pool.page_stride * es; a.head_bytes = a.pool.head_stride * es; a.slot_bytes = a.pool.slot_stride * es;
+  if (dtype == FC_F32) return launch_paged_fma(a, hd, st);
+  return hd == 128 ? launch_hd<128>(a, st) : hd == 64 ? launch_hd<64>(a, st) : launch_hd<32>(a, st);
 }
 
 }  // namespace fc

@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       if (!ok) break;
       // ---- the groups' results: the second hands over, the first adds up and writes
       const bool whole = seg_n == seg.k.n;
-      float *part = a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * (kQueries * (HD + 2));
+      float *part = a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * part_floats(kQueries, HD);
       float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + row * HD;
 #pragma unroll
       for (int c0 = 0; c0 < HD; c0 += 64, ++exchanges) {
@@ -450,7 +450,7 @@ size_t status_bytes() { return (kWorkers * sizeof(unsigned int) + 255) / 256 * 2
 
 }  // namespace
 
-size_t paged_umma_scratch(int hd) { return status_bytes() + (size_t)kWorkers * 2 * kQueries * (hd + 2) * sizeof(float); }
+size_t paged_umma_scratch(int hd) { return status_bytes() + (size_t)kWorkers * 2 * part_floats(kQueries, hd) * sizeof(float); }
 
 cudaError_t launch_paged_umma(PagedAttnArgs a, int hd, cudaStream_t st) {
   a.groups = (a.hq / a.pool.n_kv_heads * a.c + kQueries - 1) / kQueries;

@@ -1,6 +1,7 @@
 """Paged K/V cache without a GPU: calls that are refused before anything is launched, scratch sizes, the index arithmetic of the kernels."""
 import ctypes as C
 import os
+import random
 import subprocess
 
 import pytest
@@ -205,3 +206,109 @@ def test_pages_released_under_a_window_are_those_that_no_later_row_sees(host):
 
 def test_lengths_stay_within_the_table(host):
     assert [host.clamp_len(n, 100) for n in (-2 ** 31, -1, 0, 99, 100, 101, 2 ** 31 - 1)] == [-1, -1, 0, 99, 100, 100, 100]
+
+
+@pytest.fixture(scope="module")
+def parts(tmp_path_factory):
+    d = tmp_path_factory.mktemp("parts")
+    src, so = d / "wrap.cpp", d / "wrap.so"
+    src.write_text("""
+#include "fc_paged.h"
+extern "C" {
+int part_floats(int q, int hd) { return fc::part_floats(q, hd); }
+void key_tiles(int len, int rows, int cap, int w, int s, int keys, int *out) {
+  const fc::KeyTiles t = fc::key_tiles(len, rows, cap, w, s, keys);
+  out[0] = t.n;
+  for (int i = 0; i < t.n && i < 4000; ++i) out[1 + i] = fc::tile_key(t, i, keys);
+}
+long long chunk_of(long long total, int n) { return fc::chunk_of(total, n); }
+void unit_parts(long long begin, int n, long long chunk, int *out) { const fc::UnitParts p = fc::unit_parts(begin, n, chunk); out[0] = p.first; out[1] = p.last; }
+int part_place(long long begin, int worker, long long chunk) { return fc::part_place(begin, worker, chunk); }
+int paged_cluster(int b, int u, int cap, int c, int w, int s, int keys, int warps, int sms) { return fc::paged_cluster(b, u, cap, c, w, s, keys, warps, sms); }
+}
+""")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", build.CSRC, "-I", build.INCLUDE, str(src), "-o", str(so)])
+    lib_ = C.CDLL(str(so))
+    lib_.chunk_of.restype = C.c_longlong
+    lib_.chunk_of.argtypes = [C.c_longlong, C.c_int]
+    lib_.unit_parts.argtypes = [C.c_longlong, C.c_int, C.c_longlong, C.c_void_p]
+    lib_.part_place.argtypes = [C.c_longlong, C.c_int, C.c_longlong]
+    return lib_
+
+
+def test_parts_are_whole_16_byte_pieces(parts):
+    """Parts follow one another in scratch and are read and written 16 bytes at a time, for any number of queries."""
+    for hd in (32, 64, 128):
+        for q in range(1, 129):
+            n = parts.part_floats(q, hd)
+            assert n % 4 == 0 and n >= q * (hd + 2)
+
+
+@pytest.mark.parametrize("keys", [8, 16, 32, 64])
+def test_tiles_hold_every_key_that_is_seen_once(parts, keys):
+    r = random.Random(keys)
+    out = (C.c_int * 4001)()
+    for _ in range(3000):
+        cap = r.choice([1, 5, 100, 1000])
+        n, rows = r.choice([-1, 0, 1, r.randint(0, cap), cap, cap + 3]), r.choice([1, 2, 17, 64])
+        window = r.choice([0, 1, 3, r.randint(1, 200), 10 ** 9])
+        sinks = r.choice([0, 1, 5, r.randint(0, 100), 10 ** 9]) if window else 0
+        parts.key_tiles(min(n, cap), rows, cap, window, sinks, keys, out)
+        tiles = [out[1 + i] for i in range(out[0])]
+        if n < 0:
+            assert not tiles
+            continue
+        assert tiles == sorted(set(tiles)) and all(t % keys == 0 for t in tiles)
+        held = {t + i for t in tiles for i in range(keys)}
+        for p in range(min(n, cap), min(n, cap) + rows):
+            if p < cap:
+                assert held.issuperset(ref.visible(p, window, sinks))
+        if n < cap:                                                          # and no tile without a key that some row sees
+            seen = {t for p in range(n, min(n + rows, cap)) for t in ref.visible(p, window, sinks)}
+            whole = {t // keys for t in seen}
+            assert {t // keys for t in tiles} >= whole and len(tiles) <= len(whole) + rows // keys + 1
+
+
+def test_pieces_of_the_line_and_the_parts_of_units(parts):
+    """Every worker's piece cut at units: a unit that one worker has whole is written by it, others by the joining kernel from exactly the places
+    that the workers left their parts in."""
+    r = random.Random(5)
+    out = (C.c_int * 2)()
+    for _ in range(500):
+        units = [r.choice([1, 2, 7, 100, 1000]) for _ in range(r.randint(1, 60))]
+        workers, total = r.choice([1, 3, 148]), sum(units)
+        chunk = parts.chunk_of(total, workers)
+        begin, starts = 0, []
+        for n in units:
+            starts.append(begin)
+            begin += n
+        left = {}
+        for w in range(workers):
+            at, end = w * chunk, min(total, (w + 1) * chunk)
+            first = True
+            while at < end:
+                u = max(i for i, s in enumerate(starts) if s <= at)
+                n = min(end, starts[u] + units[u]) - at
+                if n < units[u]:
+                    left[(u, w)] = 0 if first else 1
+                at, first = at + n, False
+        for u, (s, n) in enumerate(zip(starts, units)):
+            parts.unit_parts(s, n, chunk, out)
+            have = {w: place for (v, w), place in left.items() if v == u}
+            if out[0] == out[1]:
+                assert not have
+            else:
+                assert have == {w: parts.part_place(s, w, chunk) for w in range(out[0], out[1] + 1)}
+
+
+def test_clusters_only_where_they_all_run_at_once_and_have_little_to_do(parts):
+    for batch in (1, 2, 16, 200):
+        for units in (1, 4, 32, 40, 148, 149):
+            for cap in (16, 500, 832, 4096, 100000):
+                for window in (0, 64):
+                    n = parts.paged_cluster(batch, units, cap, 4, window, 4, 16, 8, 148)
+                    assert n in (0, 1, 2, 4, 8)
+                    if n:
+                        assert batch * units * n <= 148
+                        keys = cap if not window else min(cap, window + 4 + 4 + 32)
+                        assert keys <= n * 8 * 4 * 16
