@@ -3,9 +3,9 @@
 #include <stdint.h>
 
 #if defined(__CUDACC__)
-#define FC_HD __host__ __device__ __forceinline__
+#define FC_ANY __host__ __device__ __forceinline__
 #else
-#define FC_HD inline
+#define FC_ANY inline
 #endif
 
 namespace fc {
@@ -33,10 +33,10 @@ struct PagedAttnArgs {
 };
 
 // Length of a sequence as the kernels use it: -1 for none, never far beyond the table's `cap` positions (no sum overflows).
-FC_HD int clamp_len(int len, int cap) { return len < 0 ? -1 : len > cap ? cap : len; }
+FC_ANY int clamp_len(int len, int cap) { return len < 0 ? -1 : len > cap ? cap : len; }
 
 // Page of position t, -1 if there is none in the pool.  row: the sequence's entries of the table.
-FC_HD int page_of(const int32_t *row, int width, int t, int page_size, int n_pages) {
+FC_ANY int page_of(const int32_t *row, int width, int t, int page_size, int n_pages) {
   if (t < 0) return -1;
   const int i = t / page_size;
   if (i >= width) return -1;
@@ -45,20 +45,20 @@ FC_HD int page_of(const int32_t *row, int width, int t, int page_size, int n_pag
 }
 
 // Whether the row at position p sees the key at position t >= 0.
-FC_HD bool sees(int p, int t, int window, int n_sink) { return t <= p && (window == 0 || t > p - window || t < n_sink); }
+FC_ANY bool sees(int p, int t, int window, int n_sink) { return t <= p && (window == 0 || t > p - window || t < n_sink); }
 
 // First position that a row at position p sees because of the window.
-FC_HD int window_first(int p, int window) { return window == 0 || p < window ? 0 : p - window + 1; }
+FC_ANY int window_first(int p, int window) { return window == 0 || p < window ? 0 : p - window + 1; }
 
 // Whether entry i of a table is released under a sliding window: no row at position len or later sees a slot of it.
-FC_HD bool page_unseen(int i, int page_size, int len, int window, int n_sink) {
+FC_ANY bool page_unseen(int i, int page_size, int len, int window, int n_sink) {
   return (long long)(i + 1) * page_size <= (long long)len - window + 1 && (long long)i * page_size >= n_sink;
 }
 
 // The keys that some of the rows at positions len .. len + rows - 1 see, in tiles of `keys` positions: tiles 0 .. sinks - 1, then
 // first .. first + n - sinks - 1.  Rows beyond the table see what is in it (their result is NaN whatever that is).
 struct KeyTiles { int n, sinks, first; };
-FC_HD KeyTiles key_tiles(int len, int rows, int cap, int window, int n_sink, int keys) {
+FC_ANY KeyTiles key_tiles(int len, int rows, int cap, int window, int n_sink, int keys) {
   KeyTiles t = {0, 0, 0};
   if (len < 0) return t;
   const int last = (len + rows < cap ? len + rows : cap) - 1;
@@ -71,17 +71,17 @@ FC_HD KeyTiles key_tiles(int len, int rows, int cap, int window, int n_sink, int
   t.n = t.sinks + last / keys - t.first + 1;
   return t;
 }
-FC_HD int tile_key(const KeyTiles &t, int i, int keys) { return (i < t.sinks ? i : t.first + i - t.sinks) * keys; }
+FC_ANY int tile_key(const KeyTiles &t, int i, int keys) { return (i < t.sinks ? i : t.first + i - t.sinks) * keys; }
 
 // All tiles of a call stand in one line: sequence by sequence, unit (kv head, group of queries) by unit, and each of `workers` takes
 // `chunk` of them in a row.  The parts of the unit at [begin, begin + n) and where worker i left its part: place 0 for what a
 // worker begins with, 1 for what it ends with.
 // A part: [queries][hd] sums, then [queries] (max, sum), in whole 16-byte pieces (sums are written and read four at a time).
-FC_HD constexpr int part_floats(int queries, int hd) { return queries * hd + (2 * queries + 3) / 4 * 4; }
+FC_ANY constexpr int part_floats(int queries, int hd) { return queries * hd + (2 * queries + 3) / 4 * 4; }
 struct UnitParts { int first, last; };
-FC_HD long long chunk_of(long long total, int workers) { return (total + workers - 1) / workers; }
-FC_HD UnitParts unit_parts(long long begin, int n, long long chunk) { return {(int)(begin / chunk), (int)((begin + n - 1) / chunk)}; }
-FC_HD int part_place(long long begin, int worker, long long chunk) { return begin > worker * chunk; }
+FC_ANY long long chunk_of(long long total, int workers) { return (total + workers - 1) / workers; }
+FC_ANY UnitParts unit_parts(long long begin, int n, long long chunk) { return {(int)(begin / chunk), (int)((begin + n - 1) / chunk)}; }
+FC_ANY int part_place(long long begin, int worker, long long chunk) { return begin > worker * chunk; }
 
 // CTAs of a cluster per unit where one launch of clusters does the work of the line and the kernel that joins its parts, 0 otherwise.  All
 // clusters have to run at once, and no warp may have more than a few tiles, whatever the lengths are (only the table's bound on them is known).

@@ -4,16 +4,14 @@
 // of the first and V of the second in shared memory, P in tensor memory.  The line of tiles, here of 64 keys, and the joining of parts are those of
 // k_paged_attn.cu.  One CTA per SM, three groups of four warps:
 //   softmax (two groups): the groups take turns at the tiles.  A thread owns a query: its scores come out of tensor memory in one piece, so that maximum
-//     and sum need no exchange; probabilities go back over the scores as three bf16 parts (all 24 bits), and the product of a tile is
-//     added to the thread's output in fp32 (the tensor core's own additions are not rounded to nearest).  While one group does this the tensor core works for
-//     the other.  Where a segment ends, the groups join through shared memory.
-//   the third: one thread issues the MMAs, three warps look up pages and load tiles (cp.async), one tile each in turn, and the queries of a
-//     unit in front of its first tile.
+//     and sum need no exchange; probabilities go back as three bf16 parts (all 24 bits), and the product of a tile is added to the thread's output in
+//     fp32 (the tensor core's own additions are not rounded to nearest), a tile later, when it has long been there.  While one group does
+//     this the tensor core works for the other.  Where a segment ends, the groups join through shared memory.
+//   the third: one thread issues the MMAs; one warp loads tiles by TMA, a box per page and sub-tile (pages of whole groups of eight slots), or two
+//     load them by cp.async (any other page); one loads the queries of the units.
 // Every wait is bounded: where one runs out the CTA says so in its status word, and the joining kernel writes NaN for what it was to compute.
-//
-// Bound at hd 64 by HBM, the exponentials and the instruction issue alike (a tile: 700, 512 and about 1000 cycles), at hd 128 by the tensor core
-// (a tile's four products: 1024).
 #include "fc_paged.cuh"
+#include "fc_plan.h"
 
 namespace fc {
 
@@ -22,7 +20,7 @@ namespace {
 constexpr int kKeys = 64, kQueries = 128;
 constexpr int kThreads = 384;
 constexpr int kSoftRegs = 224, kLoadRegs = 56;           // registers a thread: 256 x 224 + 128 x 56 = 384 x 168, what the launch holds
-constexpr int kLoaders = 3;
+constexpr int kCopyWarps = 2;                            // that load tiles where TMA does not
 
 template <int HD>
 struct UmmaCfg {
@@ -31,6 +29,10 @@ struct UmmaCfg {
   static constexpr int S = HD == 64 ? 8 : 4;                       // 128 KB of tiles
   static constexpr uint32_t kQSub = kQueries * 128u, kQ = SUB * kQSub;
   static constexpr uint32_t kExchange = kQueries * 64 * 4;         // 64 columns of the output at a time
+  // tensor memory of a group, 256 columns: scores, the parts of P, the product.  At hd 128 the parts lie over the scores, so that the next scores
+  // follow the product; at hd 64 they can be made before it.
+  static constexpr bool kApart = HD == 64;
+  static constexpr uint32_t kP = kApart ? 64 : 0, kO = kApart ? 160 : 128;
   static constexpr size_t kSmem = 1024 + (size_t)S * kTile + 2 * kQ + kExchange;
 };
 
@@ -47,6 +49,15 @@ __device__ __forceinline__ uint64_t desc_v(uint32_t saddr) {
   d |= (uint64_t)1 << 46;
   d |= (uint64_t)2 << 61;
   return d;
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.b32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r != 0;
 }
 // A in tensor memory
 __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
@@ -76,13 +87,37 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
-template <int HD>
-__global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_constant__ PagedAttnArgs a) {
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)), "l"(*reinterpret_cast<unsigned long long *>(&c)));
+  return *reinterpret_cast<float2 *>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+  return *reinterpret_cast<float2 *>(&r);
+}
+__device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap *map, const int (&x)[4], uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(bar) : "memory");
+}
+
+// Tensor maps of keys and values: dimension 0 are the elements; which of 1 .. 3 are slots, heads and pages.  box: slots that one load takes.
+struct PageMaps {
+  CUtensorMap k, v;
+  int slot_dim, head_dim, page_dim, box;
+};
+
+template <int HD, bool TMA>
+__global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_constant__ PageMaps maps, const __grid_constant__ PagedAttnArgs a) {
   using C = UmmaCfg<HD>;
   constexpr int S = C::S, PER = HD / 8;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) unsigned long long full[S], empty[S], q_free[2], s_ready[2], p_ready[2], o_ready[2], ex_full, ex_free, drained, odd_bar[2];
+  __shared__ __align__(8) unsigned long long full[S], empty[S], q_full[2], q_free[2], s_ready[2], s_free[2], p_ready[2], o_ready[2], ex_full, ex_free,
+      drained, odd_bar[2];
   __shared__ unsigned int tmem_base_s, bad_keys[S][2], odd_keys[2][2];
   __shared__ int gave_up;
   __shared__ float2 ml[kQueries];
@@ -93,18 +128,15 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   const uint32_t q_base = base + S * C::kTile;
   float4 *exchange = reinterpret_cast<float4 *>(base_g + S * C::kTile + 2 * C::kQ);      // piece c4 of row r at r * 16 + (c4 ^ (r & 15))
 
-  long long total, unused;
-  count_tiles<kKeys>(a, 0, total, unused);
-  const long long chunk = chunk_of(total, gridDim.x), f0 = chunk * blockIdx.x;
-  if (f0 >= total) return;
-  const int n_mine = (int)(total - f0 < chunk ? total - f0 : chunk);
-  Place seg = find_place<kKeys>(a, f0);
+  Place seg;
+  int n_mine;
+  if (!my_piece<kKeys, true>(a, seg, n_mine)) return;
 
   if (tid == 0) {
     for (int i = 0; i < S; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&q_free[i]), 1); mbar_init(smem_u32(&s_ready[i]), 1); mbar_init(smem_u32(&o_ready[i]), 1);
-      mbar_init(smem_u32(&p_ready[i]), 128); mbar_init(smem_u32(&odd_bar[i]), 128);
+      mbar_init(smem_u32(&q_full[i]), 1); mbar_init(smem_u32(&q_free[i]), 1); mbar_init(smem_u32(&s_ready[i]), 1); mbar_init(smem_u32(&o_ready[i]), 1);
+      mbar_init(smem_u32(&s_free[i]), 128); mbar_init(smem_u32(&p_ready[i]), 128); mbar_init(smem_u32(&odd_bar[i]), 128);
       odd_keys[i][0] = odd_keys[i][1] = 0u;
     }
     mbar_init(smem_u32(&ex_full), 128); mbar_init(smem_u32(&ex_free), 128); mbar_init(smem_u32(&drained), 1);
@@ -113,9 +145,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
     fence_proxy_async();
   }
   if (warp == 8) tmem_alloc(smem_u32(&tmem_base_s), 512);
+  tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_base_s;                     // group w: scores, then the parts of P, at column 256 w; the product at 256 w + 128
+  const uint32_t tmem = tmem_base_s;                     // group w from column 256 w
   volatile int *quit = &gave_up;
   const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
@@ -124,60 +157,158 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
     if (warp == 8) {
       // ------------------------------------------------------------------------------------------ MMAs
-      if (lane == 0) {
-        constexpr uint32_t id_s = make_idesc(kKeys), id_o = make_idesc(HD) | (1u << 16);       // V: N adjacent
-        Place at = seg;
-        int so = 0;                                      // ordinal of the segment
-        bool ok = true;
-        auto qk = [&](int i) {
-          const int st = i % S, w = i & 1;
-          if (!mbar_wait(smem_u32(&full[st]), (uint32_t)(i / S) & 1u, quit)) { ok = false; return; }
-          tc_fence_after();
-          const uint32_t qb = q_base + (uint32_t)(so & 1) * C::kQ, kb = base + st * C::kTile;
+      // The warp runs as one, on values that are broadcast from its first lane, and one thread is elected to issue: descriptors are then worked out
+      // once per warp in uniform registers.  (Inside `if (lane == 0)` an MMA cost the issuing thread about 60 cycles.)
+      constexpr uint32_t id_s = make_idesc(kKeys), id_o = make_idesc(HD) | (1u << 16);           // V: N adjacent
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), tiles = __shfl_sync(0xffffffffu, base, 0), qs = tiles + S * C::kTile;
+      const int n_all = __shfl_sync(0xffffffffu, n_mine, 0);
+      Place at = seg;
+      int so = 0;                                        // ordinal of the segment
+      bool ok = true, first = true;
+      auto qk = [&](int i) {
+        const int st = i % S, w = i & 1;
+        if (first && !mbar_wait_warp(smem_u32(&q_full[so & 1]), (uint32_t)(so >> 1) & 1u, quit)) { ok = false; return; }
+        if (!mbar_wait_warp(smem_u32(&full[st]), (uint32_t)(i / S) & 1u, quit)) { ok = false; return; }
+        tc_fence_after();
+        const uint64_t qd = smem_desc_sw128(qs + (uint32_t)(so & 1) * C::kQ), kd = smem_desc_sw128(tiles + st * C::kTile);
+        const bool next = i + 1 >= n_all || __shfl_sync(0xffffffffu, move_on<kKeys>(a, at, 1), 0) > 0;
+        if (elect_one()) {
 #pragma unroll
-          for (int ks = 0; ks < HD / 16; ++ks)
-            umma_bf16(tmem + w * 256, smem_desc_sw128(qb + (ks >> 2) * C::kQSub + (ks & 3) * 32), smem_desc_sw128(kb + (ks >> 2) * C::kSub + (ks & 3) * 32),
-                      id_s, ks > 0);
+          for (int ks = 0; ks < HD / 16; ++ks)           // descriptors count in 16 bytes
+            umma_bf16(tm + w * 256, qd + ((ks >> 2) * C::kQSub + (ks & 3) * 32) / 16, kd + ((ks >> 2) * C::kSub + (ks & 3) * 32) / 16, id_s, ks > 0);
           umma_commit(smem_u32(&s_ready[w]));
-          const int moved = i + 1 < n_mine ? move_on<kKeys>(a, at, 1) : 1;
-          if (moved) { umma_commit(smem_u32(&q_free[so & 1])); ++so; }
-        };
-        qk(0);
-        if (ok && n_mine > 1) qk(1);
-        for (int i = 0; i < n_mine && ok; ++i) {
-          const int st = i % S, w = i & 1;
-          if (!mbar_wait(smem_u32(&p_ready[w]), (uint32_t)(i >> 1) & 1u, quit)) break;
-          tc_fence_after();
-          const uint32_t vb = base + st * C::kTile + C::kHalf;
+          if (next) umma_commit(smem_u32(&q_free[so & 1]));
+        }
+        __syncwarp();
+        first = next;
+        so += next;
+      };
+      qk(0);
+      if (ok && n_all > 1) qk(1);
+      for (int i = 0; i < n_all && ok; ++i) {
+        const int st = i % S, w = i & 1;
+        const uint32_t turn = (uint32_t)(i >> 1) & 1u;
+        if (C::kApart && i + 2 < n_all) {
+          if (!mbar_wait_warp(smem_u32(&s_free[w]), turn, quit)) break;
+          qk(i + 2);
+          if (!ok) break;
+        }
+        if (!mbar_wait_warp(smem_u32(&p_ready[w]), turn, quit)) break;
+        tc_fence_after();
+        const uint64_t vd = desc_v(tiles + st * C::kTile + C::kHalf);
+        if (elect_one()) {
 #pragma unroll
           for (int part = 2; part >= 0; --part)
 #pragma unroll
             for (int ks = 0; ks < kKeys / 16; ++ks)
-              umma_bf16_ts(tmem + w * 256 + 128, tmem + w * 256 + part * 32 + ks * 8, desc_v(vb + ks * 2048), id_o, part < 2 || ks > 0);
+              umma_bf16_ts(tm + w * 256 + C::kO, tm + w * 256 + C::kP + part * 32 + ks * 8, vd + ks * 128, id_o, part < 2 || ks > 0);
           umma_commit(smem_u32(&o_ready[w]));
           umma_commit(smem_u32(&empty[st]));
-          if (i + 2 < n_mine) qk(i + 2);
         }
-        // everything issued has completed, and its arrivals are made, before shared and tensor memory are given up
-        umma_commit(smem_u32(&drained));
-        const unsigned long long t0 = clock64();
-        while (!mbar_try(smem_u32(&drained), 0))
-          if ((unsigned long long)(clock64() - t0) > kSpinBudget) { *quit = 1; break; }
+        __syncwarp();
+        if (!C::kApart && i + 2 < n_all) qk(i + 2);
       }
+      // everything issued has completed, and its arrivals are made, before shared and tensor memory are given up
+      if (elect_one()) umma_commit(smem_u32(&drained));
       __syncwarp();
+      const unsigned long long t0 = clock64();
+      while (!mbar_try(smem_u32(&drained), 0))
+        if ((unsigned long long)(clock64() - t0) > kSpinBudget) { *quit = 1; break; }
+      __syncwarp();
+    } else if (warp == 11) {
+      // ------------------------------------------------------------------------------------------ queries, a unit at a time into two buffers
+      Place at = seg;
+      for (int so = 0, done = 0; done < n_mine; ++so) {
+        if (so >= 2 && !mbar_wait_warp(smem_u32(&q_free[so & 1]), (uint32_t)((so >> 1) - 1) & 1u, quit)) break;
+        const uint32_t qb = q_base + (uint32_t)(so & 1) * C::kQ;
+        const __nv_bfloat16 *from = (const __nv_bfloat16 *)a.q + (long long)at.b * a.c * a.q_stride + (long long)at.kvh * group * HD;
+#pragma unroll 1
+        for (int r0 = 0; r0 < kQueries; r0 += 32) {      // a lane's row, then the warp goes over the pieces of 32 rows
+          const int q = min(at.qg * kQueries + r0 + lane, nq - 1), j = q / group;
+          const long long off = j * a.q_stride + (q - j * group) * HD;
+#pragma unroll 4
+          for (int y = 0; y < PER; ++y) {
+            const int r = y * (32 / PER) + lane / PER;
+            copy16(qb + uoff(kQueries, r0 + r, lane % PER), from + __shfl_sync(0xffffffffu, off, r) + (lane % PER) * 8, 16u);
+          }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&q_full[so & 1]));
+        const int n = min(n_mine - done, at.k.n - at.t);
+        done += n;
+        if (done < n_mine) move_on<kKeys>(a, at, n);
+      }
+    } else if (TMA) {
+      // ------------------------------------------------------------------------------------------ tiles by TMA: a lane per box
+      if (warp == 9) {
+        Place ld = seg;
+        const int boxes = kKeys / maps.box;
+        int i = 0, page = -2, slot = 0;                  // the lane's box: -2, no row sees it, it is not loaded; -1: nor one without a page
+        auto look_up = [&]() {                           // a tile ahead of its use
+          const int see_from = window_first(ld.len + ld.qg * kQueries / group, a.window);
+          const int see_to = min(ld.len + min(nq - 1, ld.qg * kQueries + kQueries - 1) / group, a.cap - 1);
+          const int t = tile_key(ld.k, ld.t, kKeys) + lane * maps.box;
+          page = -2;
+          if (lane < boxes && t <= see_to && (t + maps.box > see_from || t < a.n_sink)) {
+            const int e = t / a.pool.page_size;
+            slot = t - e * a.pool.page_size;
+            page = max(-1, a.table[(long long)ld.b * a.width + e]);
+          }
+        };
+        look_up();
+        for (; i < n_mine; ++i) {
+          const int st = i % S, kvh = ld.kvh, my_slot = slot, my_page = page >= a.pool.n_pages ? -1 : page;
+          if (i + 1 < n_mine) {
+            move_on<kKeys>(a, ld, 1);
+            look_up();
+          }
+          unsigned int bad = __ballot_sync(0xffffffffu, my_page == -1);
+          const int n = __popc(__ballot_sync(0xffffffffu, my_page >= 0));
+          if (i >= S && !mbar_wait_warp(smem_u32(&empty[st]), (uint32_t)(i / S - 1) & 1u, quit)) break;
+          const uint32_t bar = smem_u32(&full[st]);
+          if (lane == 0) {
+            unsigned long long keys = 0;
+            for (; bad; bad &= bad - 1) keys |= (~0ull >> (64 - maps.box)) << ((__ffs(bad) - 1) * maps.box);
+            bad_keys[st][0] = (unsigned int)keys;
+            bad_keys[st][1] = (unsigned int)(keys >> 32);
+            mbar_expect_tx(bar, (uint32_t)(n * maps.box) * (HD * 4u));
+          }
+          __syncwarp();
+          if (my_page >= 0) {
+            const uint32_t dst = base + st * C::kTile + (uint32_t)(lane * maps.box) * 128u;
+            int x[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int d = 1; d < 4; ++d) x[d] = d == maps.slot_dim ? my_slot : d == maps.head_dim ? kvh : my_page;
+#pragma unroll
+            for (int s = 0; s < C::SUB; ++s) {
+              x[0] = s * 64;
+              load_4d(dst + s * C::kSub, &maps.k, x, bar);
+              load_4d(dst + C::kHalf + s * C::kSub, &maps.v, x, bar);
+            }
+          }
+        }
+        if (i < n_mine) {                                // gave up: wait (bounded) for what was requested
+          const unsigned long long t0 = clock64();
+          for (int k = 0; k < S && k < i; ++k)
+            while (!mbar_try(smem_u32(&full[k]), last_copy_parity(i, S, k)))
+              if ((unsigned long long)(clock64() - t0) > kSpinBudget / 4) break;
+        }
+      }
     } else {
-      // ------------------------------------------------------------------------------------------ loads
+      // ------------------------------------------------------------------------------------------ tiles by cp.async, two warps in turn
       const int lw = warp - 9;
       Place ld = seg;
-      int so = 0, pending = -1;
+      int pending = -1;
       bool ok = true;
       auto landed = [&]() {                              // the copies of `pending` are here: for the tensor core to read
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&full[pending]));
       };
-      if (lw < n_mine) so += move_on<kKeys>(a, ld, lw);
-      for (int i = lw; i < n_mine; i += kLoaders) {
+      if (lw < n_mine) move_on<kKeys>(a, ld, lw);
+      for (int i = lw; i < n_mine; i += kCopyWarps) {
         const int st = i % S;
         // ---- pages of the lanes' keys (lane, lane + 32)
         const int see_from = window_first(ld.len + ld.qg * kQueries / group, a.window);
@@ -193,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           if (seen) {
             const int e = t / a.pool.page_size, page = a.table[(long long)ld.b * a.width + e];
             missing = page < 0 || page >= a.pool.n_pages;
-            if (!missing) off[x] = (long long)page * a.pool.page_stride + (long long)(t - e * a.pool.page_size) * a.pool.slot_stride;
+            if (!missing) off[x] = (long long)page * a.page_bytes + (long long)(t - e * a.pool.page_size) * a.slot_bytes;
           }
           bad[x] = __ballot_sync(0xffffffffu, missing);
         }
@@ -205,25 +336,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           }
           if (!mbar_wait_warp(smem_u32(&empty[st]), (uint32_t)(i / S - 1) & 1u, quit)) { ok = false; break; }
         }
-        if (ld.t == 0 || i == 0) {
-          // ---- the unit's queries, behind the products of the segment that had this buffer before
-          if (so >= 2 && !__all_sync(0xffffffffu, mbar_try(smem_u32(&q_free[so & 1]), (uint32_t)((so >> 1) - 1) & 1u))) {
-            if (pending >= 0) {
-              asm volatile("cp.async.wait_group 0;" ::: "memory");
-              landed();
-              pending = -1;
-            }
-            if (!mbar_wait_warp(smem_u32(&q_free[so & 1]), (uint32_t)((so >> 1) - 1) & 1u, quit)) { ok = false; break; }
-          }
-          const uint32_t qb = q_base + (uint32_t)(so & 1) * C::kQ;
-          for (int e = lane; e < kQueries * PER; e += 32) {
-            const int r = e / PER, q = min(ld.qg * kQueries + r, nq - 1), j = q / group, h = ld.kvh * group + q - j * group;
-            copy16(qb + uoff(kQueries, r, e % PER), (const __nv_bfloat16 *)a.q + ((long long)ld.b * a.c + j) * a.q_stride + h * HD + (e % PER) * 8, 16u);
-          }
-        }
         if (lane == 0) { bad_keys[st][0] = bad[0]; bad_keys[st][1] = bad[1]; }
-        const __nv_bfloat16 *k0 = (const __nv_bfloat16 *)a.pool.k + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
-        const __nv_bfloat16 *v0 = (const __nv_bfloat16 *)a.pool.v + ld.kvh * a.pool.head_stride + (lane % PER) * 8;
+        const char *k0 = (const char *)a.pool.k + ld.kvh * a.head_bytes + (lane % PER) * 16;
+        const char *v0 = (const char *)a.pool.v + ld.kvh * a.head_bytes + (lane % PER) * 16;
         const uint32_t kb = base + st * C::kTile;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
@@ -241,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           landed();
         }
         pending = st;
-        if (i + kLoaders < n_mine) so += move_on<kKeys>(a, ld, kLoaders);
+        if (i + kCopyWarps < n_mine) move_on<kKeys>(a, ld, kCopyWarps);
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
       if (ok && pending >= 0) landed();
@@ -250,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     // -------------------------------------------------------------------------------------------- softmax
     const int w = warp >> 2, row = tid & 127;
-    const uint32_t sc = tmem + w * 256 + ((uint32_t)(warp & 3) << 21), pr = sc + 128;           // this warp's 32 lanes
+    const uint32_t sc = tmem + w * 256 + ((uint32_t)(warp & 3) << 21);                          // this warp's 32 lanes
     int i = w, done = 0, exchanges = 0;
     uint32_t odd_phase = 0;
     bool ok = true;
@@ -260,9 +375,27 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       const int pos = seg.len + j, low = window_first(pos, a.window);
       const int p_first = seg.len + q0 / group, p_last = seg.len + min(nq - 1, q0 + kQueries - 1) / group;
       const int low_last = window_first(p_last, a.window);
-      float m = -INFINITY, l = 0.f, o[HD];
+      float m = -INFINITY, l = 0.f, corr = 1.f;          // corr: what the output so far counts once the last tile's product is added
+      int last = -1;                                     // the tile whose product is not added yet
+      float2 o[HD / 2];
 #pragma unroll
-      for (int c = 0; c < HD; ++c) o[c] = 0.f;
+      for (int c = 0; c < HD / 2; ++c) o[c] = make_float2(0.f, 0.f);
+      // O = corr O + P.V of the last tile
+      auto add_product = [&]() {
+        if (last < 0) return;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&o_ready[w]), (uint32_t)(last >> 1) & 1u, quit));
+        if (!ok) return;
+        tc_fence_after();
+        const float2 f = make_float2(corr, corr);
+#pragma unroll
+        for (int c0 = 0; c0 < HD / 2; c0 += 16) {
+          float y[32];
+          tmem_ld32(sc + C::kO + c0 * 2, y);
+#pragma unroll
+          for (int c = 0; c < 16; ++c) o[c0 + c] = fma2(o[c0 + c], f, make_float2(y[2 * c], y[2 * c + 1]));
+        }
+        tc_fence_before();
+      };
       for (; i < done + seg_n; i += 2) {
         const int st = i % S;
         const uint32_t turn = (uint32_t)(i >> 1) & 1u;
@@ -271,12 +404,20 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[w]), turn, quit) && mbar_wait(smem_u32(&full[st]), (uint32_t)(i / S) & 1u, quit));
         if (!ok) break;
         tc_fence_after();
+        if (!C::kApart) {                                // scores over parts: the product in front of them is there
+          add_product();
+          if (!ok) break;
+        }
         float s[kKeys];
         tmem_ld32(sc, s);
         tmem_ld32(sc + 32, s + 32);
-        const bool masked = key0 + kKeys - 1 > p_first || (key0 < low_last && key0 + kKeys > a.n_sink);
+        if (C::kApart) {
+          tc_fence_before();
+          mbar_arrive(smem_u32(&s_free[w]));
+        }
         const unsigned int bad0 = bad_keys[st][0], bad1 = bad_keys[st][1];
-        if (masked || (bad0 | bad1)) {
+        const bool masked = key0 + kKeys - 1 > p_first || (key0 < low_last && key0 + kKeys > a.n_sink) || (bad0 | bad1);
+        if (masked) {
 #pragma unroll
           for (int k = 0; k < kKeys; ++k) {
             const int t = key0 + k;
@@ -284,24 +425,32 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
             if (t > pos || (t < low && t >= a.n_sink)) s[k] = -INFINITY;
           }
         }
-        float mx[4] = {m, s[1], s[2], s[3]};
-        mx[0] = fmaxf(mx[0], s[0]);
+        float mx[4] = {fmaxf(m, s[0]), s[1], s[2], s[3]};
 #pragma unroll
-        for (int k = 4; k < kKeys; ++k) mx[k & 3] = fmaxf(mx[k & 3], s[k]);
+        for (int k = 4; k < kKeys; k += 8)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) mx[x] = k + 4 + x < kKeys ? fmaxf(fmaxf(mx[x], s[k + x]), s[k + 4 + x]) : fmaxf(mx[x], s[k + x]);
         mx[0] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        float corr = mx[0] == m ? 1.f : ex2((m - mx[0]) * sl2);                                // first tile: 2^-inf = 0
+        float corr_now = mx[0] == m ? 1.f : ex2((m - mx[0]) * sl2);                            // first tile: 2^-inf = 0
         m = mx[0];
-        const float mb = m == -INFINITY ? 0.f : m * sl2;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const float mb = m == -INFINITY ? 0.f : -m * sl2;
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int k = 0; k < kKeys; ++k) {
-          s[k] = ex2(fmaf(s[k], sl2, -mb));
-          sum[k & 3] += s[k];
+        for (int k = 0; k < kKeys; k += 2) {
+          const float2 x = fma2(make_float2(s[k], s[k + 1]), make_float2(sl2, sl2), make_float2(mb, mb));
+          s[k] = ex2(x.x);
+          s[k + 1] = ex2(x.y);
+          sum[(k >> 1) & 1] = add2(sum[(k >> 1) & 1], make_float2(s[k], s[k + 1]));
         }
-        l = fmaf(l, corr, (sum[0] + sum[1]) + (sum[2] + sum[3]));
-        // values that are not finite, in a tile that some rows see more of than others: those keys are added row by row and
-        // taken out of the tile (a probability of zero would carry them to rows that do not see them)
-        if (masked && p_first != p_last) {
+        sum[0] = add2(sum[0], sum[1]);
+        l = fmaf(l, corr_now, sum[0].x + sum[0].y);
+        if (C::kApart) {
+          add_product();
+          if (!ok) break;
+        }
+        // values that are not finite, in a tile that some row does not see whole (by TMA its unseen slots hold anything): those keys are
+        // added row by row and taken out of the tile (a probability of zero would carry them to rows that do not see them)
+        if (masked) {
           const uint32_t vb = base + st * C::kTile + C::kHalf;
           unsigned char *vg = base_g + (vb - base);
           unsigned int odd0 = 0, odd1 = 0;
@@ -324,8 +473,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           odd1 = *(volatile unsigned int *)&odd_keys[w][1];
           if (odd0 | odd1) {
 #pragma unroll
-            for (int c = 0; c < HD; ++c) o[c] *= corr;
-            corr = 1.f;
+            for (int c = 0; c < HD / 2; ++c) { o[c].x *= corr_now; o[c].y *= corr_now; }
+            corr_now = 1.f;
+#pragma unroll 1
             for (unsigned long long left = ((unsigned long long)odd1 << 32) | odd0; left; left &= left - 1) {
               const int kk = __ffsll((long long)left) - 1;
               if (!sees(pos, key0 + kk, a.window, a.n_sink)) continue;
@@ -339,8 +489,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
                 const uint32_t y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                  o[ch * 8 + 2 * c] = fmaf(p, low_half(y[c]), o[ch * 8 + 2 * c]);
-                  o[ch * 8 + 2 * c + 1] = fmaf(p, high_half(y[c]), o[ch * 8 + 2 * c + 1]);
+                  o[ch * 4 + c].x = fmaf(p, low_half(y[c]), o[ch * 4 + c].x);
+                  o[ch * 4 + c].y = fmaf(p, high_half(y[c]), o[ch * 4 + c].y);
                 }
               }
             }
@@ -356,7 +506,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
             if (row == 0) odd_keys[w][0] = odd_keys[w][1] = 0u;
           }
         }
-        // ---- probabilities in three parts, cut off (8 bits each), over the scores
+        corr = corr_now;
+        last = i;
+        // ---- probabilities in three parts, cut off (8 bits each)
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -366,39 +518,32 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
             for (int k = 0; k < 16; ++k) {
               float &p0 = s[half * 32 + 2 * k], &p1 = s[half * 32 + 2 * k + 1];
               r[k] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
-              if (part < 2) { p0 -= low_half(r[k]); p1 -= high_half(r[k]); }
+              if (part < 2) {
+                const float2 x = fma2(make_float2(low_half(r[k]), high_half(r[k])), make_float2(-1.f, -1.f), make_float2(p0, p1));
+                p0 = x.x;
+                p1 = x.y;
+              }
             }
-            tmem_st16(sc + part * 32 + half * 16, r);
+            tmem_st16(sc + C::kP + part * 32 + half * 16, r);
           }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         mbar_arrive(smem_u32(&p_ready[w]));
-        // ---- O = corr O + P.V
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&o_ready[w]), turn, quit));
-        if (!ok) break;
-        tc_fence_after();
-#pragma unroll
-        for (int c0 = 0; c0 < HD; c0 += 32) {
-          float y[32];
-          tmem_ld32(pr + c0, y);
-#pragma unroll
-          for (int c = 0; c < 32; ++c) o[c0 + c] = fmaf(o[c0 + c], corr, y[c]);
-        }
-        tc_fence_before();
       }
+      if (ok) add_product();
       if (!ok) break;
       // ---- the groups' results: the second hands over, the first adds up and writes
       const bool whole = seg_n == seg.k.n;
       float *part = a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * part_floats(kQueries, HD);
       float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + row * HD;
 #pragma unroll
-      for (int c0 = 0; c0 < HD; c0 += 64, ++exchanges) {
+      for (int c0 = 0; c0 < HD / 2; c0 += 32, ++exchanges) {
         if (w == 1) {
           if (exchanges > 0) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ex_free), (uint32_t)(exchanges - 1) & 1u, quit));
           if (!ok) break;
           if (c0 == 0) ml[row] = make_float2(m, l);
 #pragma unroll
-          for (int c = 0; c < 16; ++c) exchange[row * 16 + (c ^ (row & 15))] = make_float4(o[c0 + 4 * c], o[c0 + 4 * c + 1], o[c0 + 4 * c + 2], o[c0 + 4 * c + 3]);
+          for (int c = 0; c < 16; ++c) exchange[row * 16 + (c ^ (row & 15))] = make_float4(o[c0 + 2 * c].x, o[c0 + 2 * c].y, o[c0 + 2 * c + 1].x, o[c0 + 2 * c + 1].y);
           mbar_arrive(smem_u32(&ex_full));
         } else {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ex_full), (uint32_t)exchanges & 1u, quit));
@@ -409,9 +554,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
             const float4 x = exchange[row * 16 + (c ^ (row & 15))];
-            const float4 y = make_float4(fmaf(f1, x.x, f0 * o[c0 + 4 * c]) * f, fmaf(f1, x.y, f0 * o[c0 + 4 * c + 1]) * f,
-                                         fmaf(f1, x.z, f0 * o[c0 + 4 * c + 2]) * f, fmaf(f1, x.w, f0 * o[c0 + 4 * c + 3]) * f);
-            if (q < nq) *reinterpret_cast<float4 *>(to + c0 + 4 * c) = y;
+            const float4 y = make_float4(fmaf(f1, x.x, f0 * o[c0 + 2 * c].x) * f, fmaf(f1, x.y, f0 * o[c0 + 2 * c].y) * f,
+                                         fmaf(f1, x.z, f0 * o[c0 + 2 * c + 1].x) * f, fmaf(f1, x.w, f0 * o[c0 + 2 * c + 1].y) * f);
+            if (q < nq) *reinterpret_cast<float4 *>(to + c0 * 2 + 4 * c) = y;
           }
           if (!whole && c0 == 0 && q < nq) *reinterpret_cast<float2 *>(part + kQueries * HD + row * 2) = make_float2(M, den);
           mbar_arrive(smem_u32(&ex_free));
@@ -429,19 +574,55 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   if (tid == 0) a.status[blockIdx.x] = gave_up != 0;
 }
 
-template <int HD>
-cudaError_t launch(const PagedAttnArgs &a, cudaStream_t st) {
+// Maps of one layer's pages, dimensions by stride; false where TMA cannot load them (pages that are not whole groups of eight slots).
+using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                   const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+bool page_maps(const PagedAttnArgs &a, int hd, PageMaps *maps) {
+  if (a.pool.page_size % 8) return false;
+  static EncodeTiledFn enc = nullptr;
+  if (!enc) {
+    void *sym = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess) return false;
+    enc = (EncodeTiledFn)sym;
+  }
+  int box = 64;
+  while (a.pool.page_size % box) box /= 2;
+  struct Dim { int kind; cuuint64_t n; long long stride; } d[3] = {{0, (cuuint64_t)a.pool.page_size, a.slot_bytes}, {1, (cuuint64_t)a.pool.n_kv_heads, a.head_bytes},
+                                                                   {2, (cuuint64_t)a.pool.n_pages, a.page_bytes}};
+  for (Dim &x : d)
+    if (x.n == 1) x.stride = hd * 2;                     // its stride says nothing
+  for (int i = 0; i < 2; ++i)
+    for (int k = 0; k < 2 - i; ++k)
+      if (d[k].stride > d[k + 1].stride) { const Dim t = d[k]; d[k] = d[k + 1]; d[k + 1] = t; }
+  cuuint64_t gdim[4] = {(cuuint64_t)hd, d[0].n, d[1].n, d[2].n}, gstr[3] = {(cuuint64_t)d[0].stride, (cuuint64_t)d[1].stride, (cuuint64_t)d[2].stride};
+  cuuint32_t boxes[4] = {64, 1, 1, 1}, ones[4] = {1, 1, 1, 1};
+  maps->box = box;
+  for (int i = 0; i < 3; ++i) {
+    if (gstr[i] >= (1ull << 40)) return false;
+    if (d[i].kind == 0) { maps->slot_dim = i + 1; boxes[i + 1] = (cuuint32_t)box; }
+    if (d[i].kind == 1) maps->head_dim = i + 1;
+    if (d[i].kind == 2) maps->page_dim = i + 1;
+  }
+  for (int v = 0; v < 2; ++v)
+    if (enc(v ? &maps->v : &maps->k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, v ? a.pool.v : a.pool.k, gdim, gstr, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) return false;
+  return true;
+}
+
+template <int HD, bool TMA>
+cudaError_t launch(const PageMaps &maps, const PagedAttnArgs &a, cudaStream_t st) {
   using C = UmmaCfg<HD>;
   static bool done[kMaxDevices] = {false};
   const int dev = current_device_slot();
   if (!done[dev]) {
     // the register split is only there to be had if the launch holds what it adds up to
     cudaFuncAttributes at;
-    if (cudaError_t e = cudaFuncGetAttributes(&at, paged_umma_kernel<HD>)) return e;
+    if (cudaError_t e = cudaFuncGetAttributes(&at, paged_umma_kernel<HD, TMA>)) return e;
     if (at.numRegs * kThreads < 256 * kSoftRegs + 128 * kLoadRegs) return cudaErrorInvalidConfiguration;
-    if (cudaError_t e = allow_smem(paged_umma_kernel<HD>, C::kSmem, done)) return e;
+    if (cudaError_t e = allow_smem(paged_umma_kernel<HD, TMA>, C::kSmem, done)) return e;
   }
-  paged_umma_kernel<HD><<<kWorkers, kThreads, C::kSmem, st>>>(a);
+  paged_umma_kernel<HD, TMA><<<kWorkers, kThreads, C::kSmem, st>>>(maps, a);
   if (cudaError_t e = cudaGetLastError()) return e;
   return launch_combine<HD, kQueries, kKeys>(a, kWorkers, st);
 }
@@ -456,7 +637,10 @@ cudaError_t launch_paged_umma(PagedAttnArgs a, int hd, cudaStream_t st) {
   a.groups = (a.hq / a.pool.n_kv_heads * a.c + kQueries - 1) / kQueries;
   a.status = (unsigned int *)a.parts;
   a.parts = (float *)((char *)a.parts + status_bytes());
-  return hd == 128 ? launch<128>(a, st) : launch<64>(a, st);
+  PageMaps maps;
+  memset(&maps, 0, sizeof maps);
+  if (page_maps(a, hd, &maps)) return hd == 128 ? launch<128, true>(maps, a, st) : launch<64, true>(maps, a, st);
+  return hd == 128 ? launch<128, false>(maps, a, st) : launch<64, false>(maps, a, st);
 }
 
 }  // namespace fc
