@@ -7,8 +7,8 @@
 //     and sum need no exchange; probabilities go back as three bf16 parts (all 24 bits), and the product of a tile is added to the thread's output in
 //     fp32 (the tensor core's own additions are not rounded to nearest), a tile later, when it has long been there.  While one group does
 //     this the tensor core works for the other.  Where a segment ends, the groups join through shared memory.
-//   the third: one thread issues the MMAs; one warp loads tiles by TMA, a box per page and sub-tile (pages of whole groups of eight slots), or two
-//     load them by cp.async (any other page); one loads the queries of the units.
+//   the third: a warp issues the first product, one the second; two load tiles, keys and values by TMA, a box per page and sub-tile (pages of
+//     whole groups of eight slots), or in turn by cp.async (any other page), and the queries of a unit in front of its first tile.
 // Every wait is bounded: where one runs out the CTA says so in its status word, and the joining kernel writes NaN for what it was to compute.
 #include "fc_paged.cuh"
 #include "fc_plan.h"
@@ -67,18 +67,26 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, u
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(acc) : "memory");
 }
-// 32 columns of this thread's lane; the values are there after tmem_ld_done
+// Columns of this thread's lane.
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *v) {
   uint32_t r[32];
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr) : "memory");
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float *v) {
+  uint32_t r[64];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr) : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -116,8 +124,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   constexpr int S = C::S, PER = HD / 8;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) unsigned long long full[S], empty[S], q_full[2], q_free[2], s_ready[2], s_free[2], p_ready[2], o_ready[2], ex_full, ex_free,
-      drained, odd_bar[2];
+  __shared__ __align__(8) unsigned long long k_full[S], v_full[S], k_empty[S], v_empty[S], q_full[2], q_free[2], s_ready[2], s_free[2], p_ready[2], o_ready[2], ex_full, ex_free,
+      drained[2], odd_bar[2];
   __shared__ unsigned int tmem_base_s, bad_keys[S][2], odd_keys[2][2];
   __shared__ int gave_up;
   __shared__ float2 ml[kQueries];
@@ -133,13 +141,15 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   if (!my_piece<kKeys, true>(a, seg, n_mine)) return;
 
   if (tid == 0) {
-    for (int i = 0; i < S; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
+    for (int i = 0; i < S; ++i) {
+      mbar_init(smem_u32(&k_full[i]), 1); mbar_init(smem_u32(&v_full[i]), 1); mbar_init(smem_u32(&k_empty[i]), 1); mbar_init(smem_u32(&v_empty[i]), 1);
+    }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&q_full[i]), 1); mbar_init(smem_u32(&q_free[i]), 1); mbar_init(smem_u32(&s_ready[i]), 1); mbar_init(smem_u32(&o_ready[i]), 1);
-      mbar_init(smem_u32(&s_free[i]), 128); mbar_init(smem_u32(&p_ready[i]), 128); mbar_init(smem_u32(&odd_bar[i]), 128);
+      mbar_init(smem_u32(&s_free[i]), 128); mbar_init(smem_u32(&p_ready[i]), 128); mbar_init(smem_u32(&odd_bar[i]), 128); mbar_init(smem_u32(&drained[i]), 1);
       odd_keys[i][0] = odd_keys[i][1] = 0u;
     }
-    mbar_init(smem_u32(&ex_full), 128); mbar_init(smem_u32(&ex_free), 128); mbar_init(smem_u32(&drained), 1);
+    mbar_init(smem_u32(&ex_full), 128); mbar_init(smem_u32(&ex_free), 128);
     gave_up = 0;
     fence_barrier_init();
     fence_proxy_async();
@@ -155,45 +165,80 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
+    // Barriers of the tiles: what TMA or copies complete, and what the products free.  A warp that gives up a wait leaves its loop.
+    auto drain = [&](int k) {                            // what this warp issued has completed, its arrivals are made: then memory may be given up
+      if (elect_one()) umma_commit(smem_u32(&drained[k]));
+      __syncwarp();
+      const unsigned long long t0 = clock64();
+      while (!mbar_try(smem_u32(&drained[k]), 0))
+        if ((unsigned long long)(clock64() - t0) > kSpinBudget) { *quit = 1; break; }
+      __syncwarp();
+    };
+    // The queries of a unit into buffer `so & 1` (ordinal of the segment), behind the products of the segment that had it before.
+    auto load_queries = [&](const Place &at, int so) {
+      if (so >= 2 && !mbar_wait_warp(smem_u32(&q_free[so & 1]), (uint32_t)((so >> 1) - 1) & 1u, quit)) return false;
+      const uint32_t qb = q_base + (uint32_t)(so & 1) * C::kQ;
+      const __nv_bfloat16 *from = (const __nv_bfloat16 *)a.q + (long long)at.b * a.c * a.q_stride + (long long)at.kvh * group * HD;
+#pragma unroll 1
+      for (int r0 = 0; r0 < kQueries; r0 += 32) {        // a lane's row, then the warp goes over the pieces of 32 rows
+        const int q = min(at.qg * kQueries + r0 + lane, nq - 1), j = q / group;
+        const long long off = j * a.q_stride + (q - j * group) * HD;
+#pragma unroll 4
+        for (int y = 0; y < PER; ++y) {
+          const int r = y * (32 / PER) + lane / PER;
+          copy16(qb + uoff(kQueries, r0 + r, lane % PER), from + __shfl_sync(0xffffffffu, off, r) + (lane % PER) * 8, 16u);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&q_full[so & 1]));
+      return true;
+    };
+    // The two warps that issue MMAs run as one, on values that are broadcast from their first lane, and one thread is elected to issue:
+    // descriptors are then worked out once in uniform registers.  (Inside `if (lane == 0)` an MMA cost the issuing thread about 60 cycles.)
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), tiles = __shfl_sync(0xffffffffu, base, 0);
+    const int n_all = __shfl_sync(0xffffffffu, n_mine, 0);
     if (warp == 8) {
-      // ------------------------------------------------------------------------------------------ MMAs
-      // The warp runs as one, on values that are broadcast from its first lane, and one thread is elected to issue: descriptors are then worked out
-      // once per warp in uniform registers.  (Inside `if (lane == 0)` an MMA cost the issuing thread about 60 cycles.)
-      constexpr uint32_t id_s = make_idesc(kKeys), id_o = make_idesc(HD) | (1u << 16);           // V: N adjacent
-      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), tiles = __shfl_sync(0xffffffffu, base, 0), qs = tiles + S * C::kTile;
-      const int n_all = __shfl_sync(0xffffffffu, n_mine, 0);
+      // ------------------------------------------------------------------------------------------ S = Q.K^T
+      constexpr uint32_t id_s = make_idesc(kKeys);
+      int so = 0, left = min(n_all, seg.k.n - seg.t);    // ordinal of the segment, its tiles that are left
       Place at = seg;
-      int so = 0;                                        // ordinal of the segment
-      bool ok = true, first = true;
-      auto qk = [&](int i) {
+      bool first = true;
+      for (int i = 0; i < n_all; ++i) {
         const int st = i % S, w = i & 1;
-        if (first && !mbar_wait_warp(smem_u32(&q_full[so & 1]), (uint32_t)(so >> 1) & 1u, quit)) { ok = false; return; }
-        if (!mbar_wait_warp(smem_u32(&full[st]), (uint32_t)(i / S) & 1u, quit)) { ok = false; return; }
+        if (first && !mbar_wait_warp(smem_u32(&q_full[so & 1]), (uint32_t)(so >> 1) & 1u, quit)) break;
+        if (!mbar_wait_warp(smem_u32(&k_full[st]), (uint32_t)(i / S) & 1u, quit)) break;
+        // the scores' place: read (hd 64), or the product of the parts over it done (hd 128)
+        if (i >= 2 && !mbar_wait_warp(smem_u32(C::kApart ? &s_free[w] : &o_ready[w]), (uint32_t)((i - 2) >> 1) & 1u, quit)) break;
         tc_fence_after();
-        const uint64_t qd = smem_desc_sw128(qs + (uint32_t)(so & 1) * C::kQ), kd = smem_desc_sw128(tiles + st * C::kTile);
-        const bool next = i + 1 >= n_all || __shfl_sync(0xffffffffu, move_on<kKeys>(a, at, 1), 0) > 0;
+        const uint64_t qd = smem_desc_sw128(tiles + S * C::kTile + (uint32_t)(so & 1) * C::kQ), kd = smem_desc_sw128(tiles + st * C::kTile);
+        const bool last = --left == 0;
         if (elect_one()) {
 #pragma unroll
           for (int ks = 0; ks < HD / 16; ++ks)           // descriptors count in 16 bytes
             umma_bf16(tm + w * 256, qd + ((ks >> 2) * C::kQSub + (ks & 3) * 32) / 16, kd + ((ks >> 2) * C::kSub + (ks & 3) * 32) / 16, id_s, ks > 0);
           umma_commit(smem_u32(&s_ready[w]));
-          if (next) umma_commit(smem_u32(&q_free[so & 1]));
+          umma_commit(smem_u32(&k_empty[st]));
+          if (last) umma_commit(smem_u32(&q_free[so & 1]));
         }
         __syncwarp();
-        first = next;
-        so += next;
-      };
-      qk(0);
-      if (ok && n_all > 1) qk(1);
-      for (int i = 0; i < n_all && ok; ++i) {
-        const int st = i % S, w = i & 1;
-        const uint32_t turn = (uint32_t)(i >> 1) & 1u;
-        if (C::kApart && i + 2 < n_all) {
-          if (!mbar_wait_warp(smem_u32(&s_free[w]), turn, quit)) break;
-          qk(i + 2);
-          if (!ok) break;
+        first = last;
+        if (last && i + 1 < n_all) {
+          ++so;
+          move_on<kKeys>(a, at, min(n_all, at.k.n - at.t));
+          left = __shfl_sync(0xffffffffu, min(n_all - i - 1, at.k.n - at.t), 0);
         }
-        if (!mbar_wait_warp(smem_u32(&p_ready[w]), turn, quit)) break;
+      }
+      drain(0);
+    } else if (warp == 11) {
+      // ------------------------------------------------------------------------------------------ O = P.V
+      constexpr uint32_t id_o = make_idesc(HD) | (1u << 16);       // V: N adjacent
+      for (int i = 0; i < n_all; ++i) {
+        const int st = i % S, w = i & 1;
+        if (!mbar_wait_warp(smem_u32(&v_full[st]), (uint32_t)(i / S) & 1u, quit)) break;
+        if (!mbar_wait_warp(smem_u32(&p_ready[w]), (uint32_t)(i >> 1) & 1u, quit)) break;
         tc_fence_after();
         const uint64_t vd = desc_v(tiles + st * C::kTile + C::kHalf);
         if (elect_one()) {
@@ -203,113 +248,105 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
             for (int ks = 0; ks < kKeys / 16; ++ks)
               umma_bf16_ts(tm + w * 256 + C::kO, tm + w * 256 + C::kP + part * 32 + ks * 8, vd + ks * 128, id_o, part < 2 || ks > 0);
           umma_commit(smem_u32(&o_ready[w]));
-          umma_commit(smem_u32(&empty[st]));
+          umma_commit(smem_u32(&v_empty[st]));
         }
         __syncwarp();
-        if (!C::kApart && i + 2 < n_all) qk(i + 2);
       }
-      // everything issued has completed, and its arrivals are made, before shared and tensor memory are given up
-      if (elect_one()) umma_commit(smem_u32(&drained));
-      __syncwarp();
-      const unsigned long long t0 = clock64();
-      while (!mbar_try(smem_u32(&drained), 0))
-        if ((unsigned long long)(clock64() - t0) > kSpinBudget) { *quit = 1; break; }
-      __syncwarp();
-    } else if (warp == 11) {
-      // ------------------------------------------------------------------------------------------ queries, a unit at a time into two buffers
-      Place at = seg;
-      for (int so = 0, done = 0; done < n_mine; ++so) {
-        if (so >= 2 && !mbar_wait_warp(smem_u32(&q_free[so & 1]), (uint32_t)((so >> 1) - 1) & 1u, quit)) break;
-        const uint32_t qb = q_base + (uint32_t)(so & 1) * C::kQ;
-        const __nv_bfloat16 *from = (const __nv_bfloat16 *)a.q + (long long)at.b * a.c * a.q_stride + (long long)at.kvh * group * HD;
-#pragma unroll 1
-        for (int r0 = 0; r0 < kQueries; r0 += 32) {      // a lane's row, then the warp goes over the pieces of 32 rows
-          const int q = min(at.qg * kQueries + r0 + lane, nq - 1), j = q / group;
-          const long long off = j * a.q_stride + (q - j * group) * HD;
-#pragma unroll 4
-          for (int y = 0; y < PER; ++y) {
-            const int r = y * (32 / PER) + lane / PER;
-            copy16(qb + uoff(kQueries, r0 + r, lane % PER), from + __shfl_sync(0xffffffffu, off, r) + (lane % PER) * 8, 16u);
-          }
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&q_full[so & 1]));
-        const int n = min(n_mine - done, at.k.n - at.t);
-        done += n;
-        if (done < n_mine) move_on<kKeys>(a, at, n);
-      }
+      drain(1);
     } else if (TMA) {
-      // ------------------------------------------------------------------------------------------ tiles by TMA: a lane per box
-      if (warp == 9) {
-        Place ld = seg;
-        const int boxes = kKeys / maps.box;
-        int i = 0, page = -2, slot = 0;                  // the lane's box: -2, no row sees it, it is not loaded; -1: nor one without a page
-        auto look_up = [&]() {                           // a tile ahead of its use
-          const int see_from = window_first(ld.len + ld.qg * kQueries / group, a.window);
-          const int see_to = min(ld.len + min(nq - 1, ld.qg * kQueries + kQueries - 1) / group, a.cap - 1);
-          const int t = tile_key(ld.k, ld.t, kKeys) + lane * maps.box;
-          page = -2;
-          if (lane < boxes && t <= see_to && (t + maps.box > see_from || t < a.n_sink)) {
+      // ------------------------------------------------------------------------------------------ tiles by TMA, keys by one warp, values by the other
+      const bool keys = warp == 9;
+      unsigned long long *full = keys ? k_full : v_full, *empty = keys ? k_empty : v_empty;
+      const CUtensorMap *map = keys ? &maps.k : &maps.v;
+      Place ld = seg;
+      const int boxes = kKeys / maps.box, ahead = 32 / boxes;      // boxes of a tile; tiles whose pages the lanes look up at once
+      bool ok = true;
+      int i = 0;
+      for (int so = 0; i < n_all && ok; ++so) {          // segment by segment
+        const int seg_n = min(n_all - i, ld.k.n - ld.t);
+        if (keys && !load_queries(ld, so)) break;
+        const int see_from = window_first(ld.len + ld.qg * kQueries / group, a.window);
+        const int see_to = min(ld.len + min(nq - 1, ld.qg * kQueries + kQueries - 1) / group, a.cap - 1);
+        for (int g0 = 0; g0 < seg_n && ok; g0 += ahead) {
+          const int t = tile_key(ld.k, ld.t + g0 + lane / boxes, kKeys) + lane % boxes * maps.box;
+          int page = -2, slot = 0;                       // the lane's box: -2, no row sees it, it is not loaded; -1: nor one without a page
+          if (g0 + lane / boxes < seg_n && t <= see_to && (t + maps.box > see_from || t < a.n_sink)) {
             const int e = t / a.pool.page_size;
             slot = t - e * a.pool.page_size;
             page = max(-1, a.table[(long long)ld.b * a.width + e]);
+            if (page >= a.pool.n_pages) page = -1;
           }
-        };
-        look_up();
-        for (; i < n_mine; ++i) {
-          const int st = i % S, kvh = ld.kvh, my_slot = slot, my_page = page >= a.pool.n_pages ? -1 : page;
-          if (i + 1 < n_mine) {
-            move_on<kKeys>(a, ld, 1);
-            look_up();
-          }
-          unsigned int bad = __ballot_sync(0xffffffffu, my_page == -1);
-          const int n = __popc(__ballot_sync(0xffffffffu, my_page >= 0));
-          if (i >= S && !mbar_wait_warp(smem_u32(&empty[st]), (uint32_t)(i / S - 1) & 1u, quit)) break;
-          const uint32_t bar = smem_u32(&full[st]);
-          if (lane == 0) {
-            unsigned long long keys = 0;
-            for (; bad; bad &= bad - 1) keys |= (~0ull >> (64 - maps.box)) << ((__ffs(bad) - 1) * maps.box);
-            bad_keys[st][0] = (unsigned int)keys;
-            bad_keys[st][1] = (unsigned int)(keys >> 32);
-            mbar_expect_tx(bar, (uint32_t)(n * maps.box) * (HD * 4u));
-          }
-          __syncwarp();
-          if (my_page >= 0) {
-            const uint32_t dst = base + st * C::kTile + (uint32_t)(lane * maps.box) * 128u;
-            int x[4] = {0, 0, 0, 0};
+          const unsigned int all_bad = __ballot_sync(0xffffffffu, page == -1), all_here = __ballot_sync(0xffffffffu, page >= 0);
+          const unsigned int of_tile = boxes == 32 ? ~0u : (1u << boxes) - 1;
+          for (int g = 0; g < ahead && g0 + g < seg_n; ++g, ++i) {
+            const int st = i % S;
+            unsigned int bad = all_bad >> (g * boxes) & of_tile;
+            const unsigned int here = all_here >> (g * boxes) & of_tile;
+            if (i >= S && !mbar_wait_warp(smem_u32(&empty[st]), (uint32_t)(i / S - 1) & 1u, quit)) { ok = false; break; }
+            const uint32_t bar = smem_u32(&full[st]);
+            if (lane == 0) {
+              if (!keys) {
+                unsigned long long gone = 0;
+                for (; bad; bad &= bad - 1) gone |= (~0ull >> (64 - maps.box)) << ((__ffs(bad) - 1) * maps.box);
+                bad_keys[st][0] = (unsigned int)gone;
+                bad_keys[st][1] = (unsigned int)(gone >> 32);
+              }
+              mbar_expect_tx(bar, (uint32_t)(__popc(here) * maps.box) * (HD * 2u));
+            }
+            __syncwarp();
+            const uint32_t dst = tiles + st * C::kTile + (keys ? 0u : C::kHalf);
+            for (unsigned int left = here; left; left &= left - 1) {
+              const int b = __ffs(left) - 1;
+              const int from = __shfl_sync(0xffffffffu, slot, g * boxes + b), in = __shfl_sync(0xffffffffu, page, g * boxes + b);
+              int x[4];
 #pragma unroll
-            for (int d = 1; d < 4; ++d) x[d] = d == maps.slot_dim ? my_slot : d == maps.head_dim ? kvh : my_page;
+              for (int d = 1; d < 4; ++d) x[d] = d == maps.slot_dim ? from : d == maps.head_dim ? ld.kvh : in;
+              if (elect_one()) {
 #pragma unroll
-            for (int s = 0; s < C::SUB; ++s) {
-              x[0] = s * 64;
-              load_4d(dst + s * C::kSub, &maps.k, x, bar);
-              load_4d(dst + C::kHalf + s * C::kSub, &maps.v, x, bar);
+                for (int s = 0; s < C::SUB; ++s) {
+                  x[0] = s * 64;
+                  load_4d(dst + (uint32_t)(b * maps.box) * 128u + s * C::kSub, map, x, bar);
+                }
+              }
             }
           }
         }
-        if (i < n_mine) {                                // gave up: wait (bounded) for what was requested
-          const unsigned long long t0 = clock64();
-          for (int k = 0; k < S && k < i; ++k)
-            while (!mbar_try(smem_u32(&full[k]), last_copy_parity(i, S, k)))
-              if ((unsigned long long)(clock64() - t0) > kSpinBudget / 4) break;
-        }
+        if (i < n_all) move_on<kKeys>(a, ld, seg_n);
+      }
+      if (i < n_all) {                                   // gave up: wait (bounded) for what was requested
+        const unsigned long long t0 = clock64();
+        for (int k = 0; k < S && k < i; ++k)
+          while (!mbar_try(smem_u32(&full[k]), last_copy_parity(i, S, k)))
+            if ((unsigned long long)(clock64() - t0) > kSpinBudget / 4) break;
       }
     } else {
       // ------------------------------------------------------------------------------------------ tiles by cp.async, two warps in turn
       const int lw = warp - 9;
       Place ld = seg;
-      int pending = -1;
+      int pending = -1, so = 0;
       bool ok = true;
       auto landed = [&]() {                              // the copies of `pending` are here: for the tensor core to read
+        if (pending < 0) return;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&full[pending]));
+        if (lane == 0) { mbar_arrive(smem_u32(&k_full[pending])); mbar_arrive(smem_u32(&v_full[pending])); }
+        pending = -1;
       };
-      if (lw < n_mine) move_on<kKeys>(a, ld, lw);
+      // a wait in front of which the copies on their way are handed over: what waits for them may be what it waits for
+      auto wait_for = [&](uint32_t bar, uint32_t parity) {
+        if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        landed();
+        return mbar_wait_warp(bar, parity, quit);
+      };
+      if (lw < n_mine) so += move_on<kKeys>(a, ld, lw);
       for (int i = lw; i < n_mine; i += kCopyWarps) {
         const int st = i % S;
+        if (ld.t == 0 || i == 0) {
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          landed();
+          if (!load_queries(ld, so)) { ok = false; break; }
+        }
         // ---- pages of the lanes' keys (lane, lane + 32)
         const int see_from = window_first(ld.len + ld.qg * kQueries / group, a.window);
         const int see_to = min(ld.len + min(nq - 1, ld.qg * kQueries + kQueries - 1) / group, a.cap - 1);
@@ -328,13 +365,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           }
           bad[x] = __ballot_sync(0xffffffffu, missing);
         }
-        if (i >= S && !__all_sync(0xffffffffu, mbar_try(smem_u32(&empty[st]), (uint32_t)(i / S - 1) & 1u))) {
-          if (pending >= 0) {                            // what waits for these copies may be what frees the stage
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            landed();
-            pending = -1;
-          }
-          if (!mbar_wait_warp(smem_u32(&empty[st]), (uint32_t)(i / S - 1) & 1u, quit)) { ok = false; break; }
+        if (i >= S && (!wait_for(smem_u32(&k_empty[st]), (uint32_t)(i / S - 1) & 1u) || !wait_for(smem_u32(&v_empty[st]), (uint32_t)(i / S - 1) & 1u))) {
+          ok = false;
+          break;
         }
         if (lane == 0) { bad_keys[st][0] = bad[0]; bad_keys[st][1] = bad[1]; }
         const char *k0 = (const char *)a.pool.k + ld.kvh * a.head_bytes + (lane % PER) * 16;
@@ -351,15 +384,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
             copy16(d + C::kHalf, v0 + (o < 0 ? 0 : o), bytes);
           }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        if (pending >= 0) {
-          asm volatile("cp.async.wait_group 1;" ::: "memory");
-          landed();
-        }
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        landed();
         pending = st;
-        if (i + kCopyWarps < n_mine) move_on<kKeys>(a, ld, kCopyWarps);
+        if (i + kCopyWarps < n_mine) so += move_on<kKeys>(a, ld, kCopyWarps);
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
-      if (ok && pending >= 0) landed();
+      if (ok) landed();
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
@@ -400,8 +431,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         const int st = i % S;
         const uint32_t turn = (uint32_t)(i >> 1) & 1u;
         const int key0 = tile_key(seg.k, seg.t + i - done, kKeys);
-        // the scores; the tile's own barrier, long past, for what the loads wrote beside it
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[w]), turn, quit) && mbar_wait(smem_u32(&full[st]), (uint32_t)(i / S) & 1u, quit));
+        // the scores, and the values with what their loader wrote beside them (the keys' stage may be another tile's by now: it is free when
+        // the scores are made; the values' is not before the probabilities have been used)
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[w]), turn, quit) && mbar_wait(smem_u32(&v_full[st]), (uint32_t)(i / S) & 1u, quit));
         if (!ok) break;
         tc_fence_after();
         if (!C::kApart) {                                // scores over parts: the product in front of them is there
@@ -409,8 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           if (!ok) break;
         }
         float s[kKeys];
-        tmem_ld32(sc, s);
-        tmem_ld32(sc + 32, s + 32);
+        tmem_ld64(sc, s);
         if (C::kApart) {
           tc_fence_before();
           mbar_arrive(smem_u32(&s_free[w]));
@@ -418,12 +449,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         const unsigned int bad0 = bad_keys[st][0], bad1 = bad_keys[st][1];
         const bool masked = key0 + kKeys - 1 > p_first || (key0 < low_last && key0 + kKeys > a.n_sink) || (bad0 | bad1);
         if (masked) {
+          // bit k: whether the row sees key key0 + k (all up to `to` but those between the sinks and the window), and has a page for it
+          auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };     // bits 0 .. n - 1
+          const unsigned long long see = below(pos + 1 - key0) & ~(below(low - key0) & ~below(a.n_sink - key0));
+          const unsigned int see0 = (unsigned int)see, see1 = (unsigned int)(see >> 32);
+          if (bad0 | bad1) {
 #pragma unroll
-          for (int k = 0; k < kKeys; ++k) {
-            const int t = key0 + k;
-            if ((k < 32 ? bad0 >> k : bad1 >> (k - 32)) & 1u) s[k] = quiet_nan();
-            if (t > pos || (t < low && t >= a.n_sink)) s[k] = -INFINITY;
+            for (int k = 0; k < kKeys; ++k)
+              if ((k < 32 ? bad0 >> k : bad1 >> (k - 32)) & 1u) s[k] = quiet_nan();
           }
+#pragma unroll
+          for (int k = 0; k < kKeys; ++k)
+            if (!((k < 32 ? see0 >> k : see1 >> (k - 32)) & 1u)) s[k] = -INFINITY;
         }
         float mx[4] = {fmaxf(m, s[0]), s[1], s[2], s[3]};
 #pragma unroll
