@@ -55,42 +55,41 @@ __device__ __forceinline__ int move_on(const PagedAttnArgs &a, Place &p, int ste
   return units;
 }
 
-// Tiles of the whole call, and of the sequences in front of sequence `upto` (a warp does this together).
+// Sum over a warp, to all lanes.
+__device__ __forceinline__ int warp_sum_i(int v) { return __reduce_add_sync(0xffffffffu, v); }
+
+// Tiles of the whole line, and of the sequences in front of sequence `upto` (a warp does this together).
 template <int KEYS>
-__device__ __forceinline__ void count_tiles(const PagedAttnArgs &a, int upto, long long &total, long long &before) {
+__device__ __forceinline__ void count_tiles(const PagedAttnArgs &a, int upto, int &total, int &before) {
   const int lane = threadIdx.x & 31, units = a.groups * a.pool.n_kv_heads;
-  long long all = 0, some = 0;
+  int all = 0, some = 0;
+#pragma unroll 1
   for (int b = lane; b < a.batch; b += 32) {
     int len;
-    const long long n = (long long)seq_tiles<KEYS>(a, b, len).n * units;
+    const int n = seq_tiles<KEYS>(a, b, len).n * units;
     all += n;
     if (b < upto) some += n;
   }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    all += __shfl_xor_sync(0xffffffffu, all, o);
-    some += __shfl_xor_sync(0xffffffffu, some, o);
-  }
-  total = all;
-  before = some;
+  total = warp_sum_i(all);
+  before = warp_sum_i(some);
 }
 // The place of tile f of the line (a warp together; f is inside the line).
 template <int KEYS>
-__device__ __forceinline__ Place find_place(const PagedAttnArgs &a, long long f) {
+__device__ __forceinline__ Place find_place(const PagedAttnArgs &a, int f) {
   const int lane = threadIdx.x & 31, units = a.groups * a.pool.n_kv_heads;
-  long long base = 0;
   Place p = {0, 0, 0, 0, -1, {0, 0, 0}};
+#pragma unroll 1
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
     int len = -1;
     KeyTiles k = {0, 0, 0};
     if (b0 + lane < a.batch) k = seq_tiles<KEYS>(a, b0 + lane, len);
-    long long x = (long long)k.n * units;
+    int x = k.n * units;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
     }
-    const unsigned int beyond = __ballot_sync(0xffffffffu, base + x > f);
+    const unsigned int beyond = __ballot_sync(0xffffffffu, x > f);
     if (beyond) {
       const int w = __ffs(beyond) - 1;
       p.k.n = __shfl_sync(0xffffffffu, k.n, w);
@@ -98,14 +97,14 @@ __device__ __forceinline__ Place find_place(const PagedAttnArgs &a, long long f)
       p.k.first = __shfl_sync(0xffffffffu, k.first, w);
       p.len = __shfl_sync(0xffffffffu, len, w);
       p.b = b0 + w;
-      const long long at = f - (base + __shfl_sync(0xffffffffu, x, w) - (long long)p.k.n * units);
-      const int u = (int)(at / p.k.n);
-      p.t = (int)(at - (long long)u * p.k.n);
-      p.kvh = u / a.groups;
+      const int at = f - (__shfl_sync(0xffffffffu, x, w) - p.k.n * units);
+      const int u = (int)((unsigned int)at / (unsigned int)p.k.n);
+      p.t = at - u * p.k.n;
+      p.kvh = (int)((unsigned int)u / (unsigned int)a.groups);
       p.qg = u - p.kvh * a.groups;
       return p;
     }
-    base += __shfl_sync(0xffffffffu, x, 31);
+    f -= __shfl_sync(0xffffffffu, x, 31);
   }
   return p;
 }
@@ -133,7 +132,7 @@ struct TileStream {
   static_assert(KEYS <= 32 && 32 % KEYS == 0 && KEYS % RPI == 0, "lanes, keys and rows");
   const PagedAttnArgs &a;
   Place at;
-  int i, n, nq, group;                                   // next tile, tiles of the piece; queries of a kv head, heads of the group
+  int i, n, nq;                                          // next tile, tiles of the piece; queries of a kv head
   int see_from, see_to;                                  // keys that some query of the unit sees: the sinks, and from .. to
   int page, slot;
   uint32_t ring;                                         // shared memory
@@ -141,8 +140,7 @@ struct TileStream {
 
   __device__ __forceinline__ TileStream(const PagedAttnArgs &args, const Place &begin, int first, int count, uint32_t smem, unsigned int *bad)
       : a(args), at(begin), i(first), n(count), page(kUnseen), slot(0), ring(smem), bad_keys(bad) {
-    group = a.hq / a.pool.n_kv_heads;
-    nq = group * a.c;
+    nq = a.nq;
     if (i < n) {
       if (LINE) move_on<KEYS>(a, at, first);
       else at.t += first;
@@ -151,14 +149,14 @@ struct TileStream {
     }
   }
   __device__ __forceinline__ void unit_keys() {
-    see_from = window_first(at.len + at.qg * QUERIES / group, a.window);                 // the first row's window reaches furthest back
-    see_to = min(at.len + min(nq - 1, at.qg * QUERIES + QUERIES - 1) / group, a.cap - 1);
+    see_from = window_first(at.len + quotient16(at.qg * QUERIES, a.group_inv), a.window);          // the first row's window reaches furthest back
+    see_to = min(at.len + quotient16(min(nq - 1, at.qg * QUERIES + QUERIES - 1), a.group_inv), a.cap - 1);
   }
   __device__ __forceinline__ void look_up() {
     const int t = tile_key(at.k, at.t, KEYS) + (threadIdx.x & (KEYS - 1));
     page = kUnseen;
     if (t <= see_to && (t >= see_from || t < a.n_sink)) {
-      const int e = t / a.pool.page_size;
+      const int e = (int)((unsigned int)t / (unsigned int)a.pool.page_size);
       slot = t - e * a.pool.page_size;
       page = max(-1, a.table[(long long)at.b * a.width + e]);
     }
@@ -201,11 +199,11 @@ struct TileStream {
 template <int KEYS, bool LINE>
 __device__ __forceinline__ bool my_piece(const PagedAttnArgs &a, Place &seg, int &n) {
   if (LINE) {
-    long long total, unused;
+    int total, unused;
     count_tiles<KEYS>(a, 0, total, unused);
-    const long long chunk = chunk_of(total, gridDim.x), f0 = chunk * blockIdx.x;
-    if (f0 >= total) return false;
-    n = (int)(total - f0 < chunk ? total - f0 : chunk);
+    const int chunk = chunk_of(total, kWorkers), f0 = chunk * (int)blockIdx.x;       // chunk x workers < 2^31 + workers
+    if (f0 >= total || f0 < 0) return false;
+    n = min(total - f0, chunk);
     seg = find_place<KEYS>(a, f0);
   } else {
     seg.b = blockIdx.z; seg.kvh = blockIdx.y / a.groups; seg.qg = blockIdx.y - seg.kvh * a.groups;
@@ -220,7 +218,7 @@ __device__ __forceinline__ bool my_piece(const PagedAttnArgs &a, Place &seg, int
 // The parts of a cluster: un-normalised sums [rows][HD] at `sums` and (max, sum) at `ml` in each CTA's shared memory.  Every CTA writes a share of the rows.
 template <int HD>
 __device__ __forceinline__ void join_cluster(const PagedAttnArgs &a, const Place &seg, int q0, int rows, uint32_t sums, uint32_t ml, int threads) {
-  const int ns = gridDim.x, group = a.hq / a.pool.n_kv_heads;
+  const int ns = gridDim.x, group = a.group;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
   cluster_sync_all();
   for (int e = blockIdx.x * threads + threadIdx.x; e < rows * (HD / 4); e += ns * threads) {
@@ -246,7 +244,7 @@ __device__ __forceinline__ void join_cluster(const PagedAttnArgs &a, const Place
       den = fmaf(mv[r].y, f, den);
       acc.x = fmaf(f, ov[r].x, acc.x); acc.y = fmaf(f, ov[r].y, acc.y); acc.z = fmaf(f, ov[r].z, acc.z); acc.w = fmaf(f, ov[r].w, acc.w);
     }
-    const int q = q0 + row, j = q / group, h = seg.kvh * group + q - j * group;
+    const int q = q0 + row, j = quotient16(q, a.group_inv), h = seg.kvh * group + q - j * group;
     const float f = seg.len < 0 ? 0.f : result_scale(a, seg.len + j, den);
     *reinterpret_cast<float4 *>(a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD + c4 * 4) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
   }
@@ -259,24 +257,24 @@ __device__ __forceinline__ void join_cluster(const PagedAttnArgs &a, const Place
 constexpr int kCombine = 256;
 
 template <int HD, int Q, int KEYS>
-__global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_constant__ PagedAttnArgs a, int workers, int block_rows) {
-  __shared__ long long counts[2];
+__global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_constant__ PagedAttnArgs a, int block_rows) {
+  __shared__ int counts[2];
   __shared__ float4 acc_s[kCombine];
   __shared__ float2 ml_s[kCombine];
   const int units = a.groups * a.pool.n_kv_heads, b = blockIdx.x / units, u = blockIdx.x - b * units, tid = threadIdx.x;
   int len;
   const KeyTiles k = seq_tiles<KEYS>(a, b, len);
   if (tid < 32) {
-    long long total, before;
+    int total, before;
     count_tiles<KEYS>(a, b, total, before);
     if (tid == 0) { counts[0] = total; counts[1] = before; }
   }
   __syncthreads();
-  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c;
+  const int group = a.group, nq = a.nq;
   const int kvh = u / a.groups, q0 = (u - kvh * a.groups) * Q, row0 = blockIdx.y * block_rows;
   const int n_rows = min(block_rows, min(Q, nq - q0) - row0), items = n_rows * (HD / 4);
   if (n_rows <= 0) return;
-  const long long chunk = chunk_of(counts[0], workers), begin = counts[1] + (long long)u * k.n;
+  const int chunk = chunk_of(counts[0], kWorkers), begin = counts[1] + u * k.n;
   UnitParts w = {0, -1};
   if (k.n > 0) {
     w = unit_parts(begin, k.n, chunk);
@@ -346,19 +344,19 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
       }
     }
     if (e < items && g == 0) {
-      const int q = q0 + row0 + row, j = q / group, h = kvh * group + q - j * group;
+      const int q = q0 + row0 + row, j = quotient16(q, a.group_inv), h = kvh * group + q - j * group;
       const float f = lost ? quiet_nan() : len < 0 ? 0.f : result_scale(a, len + j, den);
       *reinterpret_cast<float4 *>(a.out + (((long long)b * a.c + j) * a.hq + h) * HD + c4 * 4) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
     }
   }
 }
 
-// Blocks of the launch behind a line of `workers` CTAs: whole units, or fewer queries per block while there are not enough blocks for the GPU.
+// Blocks of the launch behind the line: whole units, or fewer queries per block while there are not enough blocks for the GPU.
 template <int HD, int Q, int KEYS>
-cudaError_t launch_combine(const PagedAttnArgs &a, int workers, cudaStream_t st) {
+cudaError_t launch_combine(const PagedAttnArgs &a, cudaStream_t st) {
   const long long units = (long long)a.batch * a.groups * a.pool.n_kv_heads;
   int rows = Q < 16 ? Q : 16;
-  while (rows > 1 && units * (Q / rows) < workers) rows /= 2;
+  while (rows > 1 && units * (Q / rows) < kWorkers) rows /= 2;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = dim3((unsigned)units, Q / rows); cfg.blockDim = dim3(kCombine); cfg.stream = st;
@@ -366,7 +364,7 @@ cudaError_t launch_combine(const PagedAttnArgs &a, int workers, cudaStream_t st)
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, paged_combine_kernel<HD, Q, KEYS>, a, workers, rows);
+  return cudaLaunchKernelEx(&cfg, paged_combine_kernel<HD, Q, KEYS>, a, rows);
 }
 template <typename K>
 cudaError_t allow_smem(K kernel, size_t bytes, bool *done) {
@@ -377,17 +375,42 @@ cudaError_t allow_smem(K kernel, size_t bytes, bool *done) {
   return e;
 }
 
+// What the kernels know of a call's queries, for units of Q of them.
+inline void set_groups(PagedAttnArgs &a, int Q) {
+  a.group = a.hq / a.pool.n_kv_heads;
+  a.nq = a.group * a.c;
+  a.groups = (a.nq + Q - 1) / Q;
+  a.group_inv = reciprocal16(a.group);
+}
+// A launch for as many sequences at a time as a line can hold (all of them, but for tables of billions of positions).
+template <typename F>
+cudaError_t by_lines(const PagedAttnArgs &all, int keys, F launch) {
+  const int most = line_batch(all.groups * all.pool.n_kv_heads, all.cap, keys);
+  if (most == 0) return cudaErrorInvalidValue;
+  for (int b0 = 0; b0 < all.batch; b0 += most) {
+    PagedAttnArgs a = all;
+    a.batch = all.batch - b0 < most ? all.batch - b0 : most;
+    a.table += (long long)b0 * a.width;
+    a.kv_len += b0;
+    a.q = (const char *)a.q + (long long)b0 * a.c * a.q_stride * a.elem_bytes;
+    a.out += (long long)b0 * a.c * a.hq * all.hd;
+    if (cudaError_t e = launch(a)) return e;
+  }
+  return cudaSuccess;
+}
+
 // The line and the kernel that joins its parts, or clusters where paged_cluster says so.
 template <int HD, int Q, int KEYS, typename L, typename C>
 cudaError_t launch_units(PagedAttnArgs a, L line, C cluster, int warps, size_t smem, bool *line_done, bool *cluster_done, cudaStream_t st) {
-  const int nq = a.hq / a.pool.n_kv_heads * a.c;
-  a.groups = (nq + Q - 1) / Q;
+  set_groups(a, Q);
   const int ctas = paged_cluster(a.batch, a.groups * a.pool.n_kv_heads, a.cap, a.c, a.window, a.n_sink, KEYS, warps, kWorkers);
   if (ctas == 0) {
     if (cudaError_t e = allow_smem(line, smem, line_done)) return e;
-    line<<<kWorkers, warps * 32, smem, st>>>(a);
-    if (cudaError_t e = cudaGetLastError()) return e;
-    return launch_combine<HD, Q, KEYS>(a, kWorkers, st);
+    return by_lines(a, KEYS, [&](const PagedAttnArgs &part) {
+      line<<<kWorkers, warps * 32, smem, st>>>(part);
+      if (cudaError_t e = cudaGetLastError()) return e;
+      return launch_combine<HD, Q, KEYS>(part, st);
+    });
   }
   if (cudaError_t e = allow_smem(cluster, smem, cluster_done)) return e;
   cudaLaunchConfig_t cfg;

@@ -25,8 +25,10 @@ struct PagedAttnArgs {
   const void *q; long long q_stride;      // elements
   float *out;             // [batch * c, hq * hd]
   int batch, c, hq, window, n_sink;       // n_sink is 0 without a window
-  // set by the launcher: groups of queries of a kv head, the pool's strides in bytes
-  int groups;
+  // set by the launcher: the queries' arithmetic (reciprocal of the heads of a group), the pool's strides in bytes
+  int group, nq, groups;  // heads of a group, queries of a kv head, units of a kv head
+  unsigned int group_inv;
+  int hd, elem_bytes;
   long long page_bytes, head_bytes, slot_bytes;
   float *parts;           // scratch: two parts per worker, [queries][hd] sums and [queries] (max, sum)
   unsigned int *status;   // scratch of the kernel that has waits, else null: per worker, 1 where a wait ran out
@@ -64,24 +66,38 @@ FC_ANY KeyTiles key_tiles(int len, int rows, int cap, int window, int n_sink, in
   const int last = (len + rows < cap ? len + rows : cap) - 1;
   int low = window_first(len, window);
   if (low > last) low = last;
-  t.first = low / keys;
+  const unsigned int k = (unsigned int)keys;             // a power of two that the compiler knows, where it matters
+  t.first = (int)((unsigned int)low / k);
   const int sink_keys = window == 0 ? 0 : n_sink < low ? n_sink : low;
-  t.sinks = sink_keys / keys + (sink_keys % keys != 0);
+  t.sinks = (int)(((unsigned int)sink_keys + k - 1) / k);
   if (t.sinks > t.first) t.sinks = t.first;
-  t.n = t.sinks + last / keys - t.first + 1;
+  t.n = t.sinks + (int)((unsigned int)last / k) - t.first + 1;
   return t;
 }
 FC_ANY int tile_key(const KeyTiles &t, int i, int keys) { return (i < t.sinks ? i : t.first + i - t.sinks) * keys; }
 
-// All tiles of a call stand in one line: sequence by sequence, unit (kv head, group of queries) by unit, and each of `workers` takes
-// `chunk` of them in a row.  The parts of the unit at [begin, begin + n) and where worker i left its part: place 0 for what a
+// All tiles of a launch stand in one line (its host side sees to it that they are fewer than 2^31): sequence by sequence, unit (kv head,
+// group of queries) by unit, and each of `workers` takes `chunk` of them in a row.  The parts of the unit at [begin, begin + n) and where worker i left its part: place 0 for what a
 // worker begins with, 1 for what it ends with.
 // A part: [queries][hd] sums, then [queries] (max, sum), in whole 16-byte pieces (sums are written and read four at a time).
 FC_ANY constexpr int part_floats(int queries, int hd) { return queries * hd + (2 * queries + 3) / 4 * 4; }
 struct UnitParts { int first, last; };
-FC_ANY long long chunk_of(long long total, int workers) { return (total + workers - 1) / workers; }
-FC_ANY UnitParts unit_parts(long long begin, int n, long long chunk) { return {(int)(begin / chunk), (int)((begin + n - 1) / chunk)}; }
-FC_ANY int part_place(long long begin, int worker, long long chunk) { return begin > worker * chunk; }
+FC_ANY int chunk_of(int total, int workers) { return total / workers + (total % workers != 0); }
+FC_ANY UnitParts unit_parts(int begin, int n, int chunk) {
+  const int first = (int)((unsigned int)begin / (unsigned int)chunk);
+  return {first, first + (int)((unsigned int)(begin - first * chunk + n - 1) / (unsigned int)chunk)};
+}
+FC_ANY int part_place(int begin, int worker, int chunk) { return begin > worker * chunk; }
+
+// x / n for 0 <= x < 2^16, n < 2^16, by the reciprocal of n.
+FC_ANY unsigned int reciprocal16(int n) { return n == 1 ? 0u : (unsigned int)((0x100000000ull + (unsigned int)n - 1) / (unsigned int)n); }
+FC_ANY int quotient16(int x, unsigned int inv) { return inv ? (int)((unsigned long long)(unsigned int)x * inv >> 32) : x; }
+
+// Sequences that a launch can take: units of each in at most the table's tiles; 0 if not even one.
+inline int line_batch(int units, int cap, int keys) {
+  const long long most = (long long)units * (cap / keys + 1);
+  return most > 0x7fffffff ? 0 : (int)(0x7fffffffll / most);
+}
 
 // CTAs of a cluster per unit where one launch of clusters does the work of the line and the kernel that joins its parts, 0 otherwise.  All
 // clusters have to run at once, and no warp may have more than a few tiles, whatever the lengths are (only the table's bound on them is known).
@@ -95,5 +111,13 @@ inline int paged_cluster(int batch, int units, int cap, int c, int window, int n
 
 // Whether the kernel on tcgen05 takes a kv head's nq queries.
 inline bool paged_umma(int nq, int hd) { return nq > 32 && hd >= 64; }
+// Queries of a unit and keys of a tile in fp32 (k_paged_fma.cu) and in bf16 (k_paged_attn.cu, k_paged_umma.cu).
+inline int paged_queries(int nq, int hd, bool f32) { return f32 ? (nq == 1 ? 1 : 8) : paged_umma(nq, hd) ? 128 : nq <= 8 ? 8 : 16; }
+inline int paged_keys(int nq, int hd, bool f32) { return f32 ? 1024 / hd : paged_umma(nq, hd) ? 64 : 16; }
+// Whether one sequence's tiles can be counted.
+inline bool paged_line_fits(int nq, int n_kv_heads, int hd, bool f32, int cap) {
+  const int q = paged_queries(nq, hd, f32);
+  return line_batch(n_kv_heads * ((nq + q - 1) / q), cap, paged_keys(nq, hd, f32)) > 0;
+}
 
 }  // namespace fc

@@ -83,7 +83,7 @@ int call_ok(const fc_pages *pages, int layer, const int32_t *table, int width, c
   if (int rc = pages_ok(pages)) return rc;
   if (!table || !kv_len || layer < 0 || layer >= pages->n_layers || width < 1 || batch < 1 || c < 1 || c > 64 || hq < 1) return FC_ERR_ARG;
   if (hq % pages->n_kv_heads) return FC_ERR_ARG;
-  if ((long long)width * pages->page_size > INT_MAX - 1024 || (long long)batch * c * hq > INT_MAX / 2 || hq > 65535) return FC_ERR_CAPACITY;
+  if ((long long)width * pages->page_size > INT_MAX - 1024 || (long long)batch * c * hq > INT_MAX / 2 || hq > 512) return FC_ERR_CAPACITY;
   return FC_OK;
 }
 
@@ -146,6 +146,7 @@ extern "C" int fc_op_paged_attention(const fc_pages *pages, int32_t layer, const
   if (!q || !out || !scratch || ((uintptr_t)q | (uintptr_t)out) % 16 || (uintptr_t)scratch % 256 || q_stride % per ||
       q_stride < (int64_t)n_heads * hd || window < 0 || n_sink < 0) return FC_ERR_ARG;
   if (scratch_bytes < fc_op_paged_attention_scratch_bytes(batch, c, n_heads, pages->n_kv_heads, hd, pages->dtype)) return FC_ERR_CAPACITY;
+  if (!paged_line_fits(n_heads / pages->n_kv_heads * c, pages->n_kv_heads, hd, pages->dtype == FC_F32, table_width * pages->page_size)) return FC_ERR_CAPACITY;
   PagedAttnArgs a; memset(&a, 0, sizeof a);
   a.pool = view_of(pages, layer);
   a.table = table; a.width = table_width; a.cap = table_width * pages->page_size; a.kv_len = kv_len; a.q = q; a.q_stride = q_stride; a.out = out;

@@ -59,13 +59,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
   const uint32_t ring = base + (uint32_t)warp * (S * C::kTile);
   float4 *exchange = reinterpret_cast<float4 *>(base_g + C::kRing);
 
-  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c;
+  const int group = a.group, nq = a.nq;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
   Place seg;                                             // where the segment (a unit's tiles in this CTA's piece) begins
   int n_mine;
   if (!my_piece<kKeys, LINE>(a, seg, n_mine)) return;
   TileStream<kKeys, C::kRow, S, W, Q, LINE> stream(a, seg, warp, n_mine, ring, bad_keys[warp]);
-#pragma unroll
+#pragma unroll 1
   for (int s = 0; s < S - 1; ++s) stream.request(s);
 
   int stage = 0;
@@ -82,10 +82,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
     for (int n = 0; n < QN; ++n) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        pos[n][x] = seg.len + min(q0 + n * 8 + t4 * 2 + x, nq - 1) / group;
+        pos[n][x] = seg.len + quotient16(min(q0 + n * 8 + t4 * 2 + x, nq - 1), a.group_inv);
         low[n][x] = window_first(pos[n][x], a.window);
       }
-      const int q = min(q0 + n * 8 + g4, nq - 1), j = q / group, h = seg.kvh * group + q - j * group;
+      const int q = min(q0 + n * 8 + g4, nq - 1), j = quotient16(q, a.group_inv), h = seg.kvh * group + q - j * group;
       const __nv_bfloat16 *qr = (const __nv_bfloat16 *)a.q + ((long long)seg.b * a.c + j) * a.q_stride + h * HD + t4 * 2;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
         qf[n][ks][1] = *reinterpret_cast<const uint32_t *>(qr + ks * 16 + 8);
       }
     }
-    const int p_first = seg.len + q0 / group, p_last = seg.len + q_last / group;
+    const int p_first = seg.len + quotient16(q0, a.group_inv), p_last = seg.len + quotient16(q_last, a.group_inv);
     const int low_last = window_first(p_last, a.window);
     float m_run[QN][2], l_run[QN][2], o[QN][DB][4];
 #pragma unroll
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
         for (int x = 0; x < 2; ++x) {
           const int q = q0 + n * 8 + t4 * 2 + x;
           if (q >= nq) continue;
-          const int j = q / group, h = seg.kvh * group + q - j * group;
+          const int j = quotient16(q, a.group_inv), h = seg.kvh * group + q - j * group;
           const float f = !whole ? 1.f : seg.len < 0 ? 0.f : result_scale(a, pos[n][x], den[x]);
           float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + (q - q0) * HD;
           to[d * 16 + g4] = sum[x] * f;
@@ -350,6 +350,7 @@ size_t paged_attn_scratch(int nq, int hd, int dtype) {
 
 cudaError_t launch_paged_attn(PagedAttnArgs a, int dtype, int hd, cudaStream_t st) {
   const int es = dtype == FC_F32 ? 4 : 2;
+  a.hd = hd; a.elem_bytes = es;
   a.page_bytes = a.pool.page_stride * es; a.head_bytes = a.pool.head_stride * es; a.slot_bytes = a.pool.slot_stride * es;
   if (dtype == FC_F32) return launch_paged_fma(a, hd, st);
   return hd == 128 ? launch_hd<128>(a, st) : hd == 64 ? launch_hd<64>(a, st) : launch_hd<32>(a, st);

@@ -40,13 +40,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
   float *ps = qs + QB * HD + warp * KEYS * QB;
   float *exchange = qs + QB * HD + W * KEYS * QB;
 
-  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c;
+  const int group = a.group, nq = a.nq;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
   Place seg;
   int n_mine;
   if (!my_piece<KEYS, LINE>(a, seg, n_mine)) return;
   TileStream<KEYS, C::kRow, S, W, QB, LINE> stream(a, seg, warp, n_mine, ring, bad_keys[warp]);
-#pragma unroll
+#pragma unroll 1
   for (int s = 0; s < S - 1; ++s) stream.request(s);
 
   const int key = lane % KEYS, share = lane / KEYS;      // a lane's key, and which 32 elements of it
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
     const int seg_n = min(n_mine - done, seg.k.n - seg.t);
     const int q0 = seg.qg * QB, q_last = min(nq - 1, q0 + QB - 1);
     for (int e = tid; e < QB * (HD / 4); e += kThreads) {
-      const int n = e / (HD / 4), c4 = e - n * (HD / 4), q = min(q0 + n, nq - 1), j = q / group, h = seg.kvh * group + q - j * group;
+      const int n = e / (HD / 4), c4 = e - n * (HD / 4), q = min(q0 + n, nq - 1), j = quotient16(q, a.group_inv), h = seg.kvh * group + q - j * group;
       reinterpret_cast<float4 *>(qs)[e] = *reinterpret_cast<const float4 *>((const float *)a.q + ((long long)seg.b * a.c + j) * a.q_stride + h * HD + c4 * 4);
     }
     __syncthreads();
@@ -64,13 +64,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
     float m[QB], l[QB], o[QB][E];
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
-      pos[n] = seg.len + min(q0 + n, nq - 1) / group;
+      pos[n] = seg.len + quotient16(min(q0 + n, nq - 1), a.group_inv);
       m[n] = -INFINITY;
       l[n] = 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e) o[n][e] = 0.f;
     }
-    const int p_first = seg.len + q0 / group, p_last = seg.len + q_last / group, low_last = window_first(p_last, a.window);
+    const int p_first = seg.len + quotient16(q0, a.group_inv), p_last = seg.len + quotient16(q_last, a.group_inv), low_last = window_first(p_last, a.window);
 
     for (; i < done + seg_n; i += W) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
         for (int e = 0; e < E; ++e) exchange[(warp * C::XQ + n) * HD + lane * E + e] = o[n0 + n][e];
       __syncthreads();
       for (int e = tid; e < C::XQ * (HD / 4); e += kThreads) {
-        const int x = e / (HD / 4), c4 = e - x * (HD / 4), n = n0 + x, q = q0 + n, j = q / group, h = seg.kvh * group + q - j * group;
+        const int x = e / (HD / 4), c4 = e - x * (HD / 4), n = n0 + x, q = q0 + n, j = quotient16(q, a.group_inv), h = seg.kvh * group + q - j * group;
         if (q >= nq) continue;
         float M = -INFINITY, den = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);

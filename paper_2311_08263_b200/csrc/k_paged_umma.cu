@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;                     // group w from column 256 w
   volatile int *quit = &gave_up;
-  const int group = a.hq / a.pool.n_kv_heads, nq = group * a.c;
+  const int group = a.group, nq = a.nq;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
 
   if (warp >= 8) {
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       const __nv_bfloat16 *from = (const __nv_bfloat16 *)a.q + (long long)at.b * a.c * a.q_stride + (long long)at.kvh * group * HD;
 #pragma unroll 1
       for (int r0 = 0; r0 < kQueries; r0 += 32) {        // a lane's row, then the warp goes over the pieces of 32 rows
-        const int q = min(at.qg * kQueries + r0 + lane, nq - 1), j = q / group;
+        const int q = min(at.qg * kQueries + r0 + lane, nq - 1), j = quotient16(q, a.group_inv);
         const long long off = j * a.q_stride + (q - j * group) * HD;
 #pragma unroll 4
         for (int y = 0; y < PER; ++y) {
@@ -265,13 +265,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       for (int so = 0; i < n_all && ok; ++so) {          // segment by segment
         const int seg_n = min(n_all - i, ld.k.n - ld.t);
         if (keys && !load_queries(ld, so)) break;
-        const int see_from = window_first(ld.len + ld.qg * kQueries / group, a.window);
-        const int see_to = min(ld.len + min(nq - 1, ld.qg * kQueries + kQueries - 1) / group, a.cap - 1);
+        const int see_from = window_first(ld.len + quotient16(ld.qg * kQueries, a.group_inv), a.window);
+        const int see_to = min(ld.len + quotient16(min(nq - 1, ld.qg * kQueries + kQueries - 1), a.group_inv), a.cap - 1);
         for (int g0 = 0; g0 < seg_n && ok; g0 += ahead) {
           const int t = tile_key(ld.k, ld.t + g0 + lane / boxes, kKeys) + lane % boxes * maps.box;
           int page = -2, slot = 0;                       // the lane's box: -2, no row sees it, it is not loaded; -1: nor one without a page
           if (g0 + lane / boxes < seg_n && t <= see_to && (t + maps.box > see_from || t < a.n_sink)) {
-            const int e = t / a.pool.page_size;
+            const int e = (int)((unsigned int)t / (unsigned int)a.pool.page_size);
             slot = t - e * a.pool.page_size;
             page = max(-1, a.table[(long long)ld.b * a.width + e]);
             if (page >= a.pool.n_pages) page = -1;
@@ -348,8 +348,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           if (!load_queries(ld, so)) { ok = false; break; }
         }
         // ---- pages of the lanes' keys (lane, lane + 32)
-        const int see_from = window_first(ld.len + ld.qg * kQueries / group, a.window);
-        const int see_to = min(ld.len + min(nq - 1, ld.qg * kQueries + kQueries - 1) / group, a.cap - 1);
+        const int see_from = window_first(ld.len + quotient16(ld.qg * kQueries, a.group_inv), a.window);
+        const int see_to = min(ld.len + quotient16(min(nq - 1, ld.qg * kQueries + kQueries - 1), a.group_inv), a.cap - 1);
         long long off[2];
         unsigned int bad[2];
 #pragma unroll
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           off[x] = -1;
           bool missing = false;
           if (seen) {
-            const int e = t / a.pool.page_size, page = a.table[(long long)ld.b * a.width + e];
+            const int e = (int)((unsigned int)t / (unsigned int)a.pool.page_size), page = a.table[(long long)ld.b * a.width + e];
             missing = page < 0 || page >= a.pool.n_pages;
             if (!missing) off[x] = (long long)page * a.page_bytes + (long long)(t - e * a.pool.page_size) * a.slot_bytes;
           }
@@ -402,9 +402,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
     bool ok = true;
     while (ok) {
       const int seg_n = min(n_mine - done, seg.k.n - seg.t);
-      const int q0 = seg.qg * kQueries, q = q0 + row, qc = min(q, nq - 1), j = qc / group, h = seg.kvh * group + qc - j * group;
+      const int q0 = seg.qg * kQueries, q = q0 + row, qc = min(q, nq - 1), j = quotient16(qc, a.group_inv), h = seg.kvh * group + qc - j * group;
       const int pos = seg.len + j, low = window_first(pos, a.window);
-      const int p_first = seg.len + q0 / group, p_last = seg.len + min(nq - 1, q0 + kQueries - 1) / group;
+      const int p_first = seg.len + quotient16(q0, a.group_inv), p_last = seg.len + quotient16(min(nq - 1, q0 + kQueries - 1), a.group_inv);
       const int low_last = window_first(p_last, a.window);
       float m = -INFINITY, l = 0.f, corr = 1.f;          // corr: what the output so far counts once the last tile's product is added
       int last = -1;                                     // the tile whose product is not added yet
@@ -659,9 +659,11 @@ cudaError_t launch(const PageMaps &maps, const PagedAttnArgs &a, cudaStream_t st
     if (at.numRegs * kThreads < 256 * kSoftRegs + 128 * kLoadRegs) return cudaErrorInvalidConfiguration;
     if (cudaError_t e = allow_smem(paged_umma_kernel<HD, TMA>, C::kSmem, done)) return e;
   }
-  paged_umma_kernel<HD, TMA><<<kWorkers, kThreads, C::kSmem, st>>>(maps, a);
-  if (cudaError_t e = cudaGetLastError()) return e;
-  return launch_combine<HD, kQueries, kKeys>(a, kWorkers, st);
+  return by_lines(a, kKeys, [&](const PagedAttnArgs &part) {
+    paged_umma_kernel<HD, TMA><<<kWorkers, kThreads, C::kSmem, st>>>(maps, part);
+    if (cudaError_t e = cudaGetLastError()) return e;
+    return launch_combine<HD, kQueries, kKeys>(part, st);
+  });
 }
 
 size_t status_bytes() { return (kWorkers * sizeof(unsigned int) + 255) / 256 * 256; }
@@ -671,7 +673,7 @@ size_t status_bytes() { return (kWorkers * sizeof(unsigned int) + 255) / 256 * 2
 size_t paged_umma_scratch(int hd) { return status_bytes() + (size_t)kWorkers * 2 * part_floats(kQueries, hd) * sizeof(float); }
 
 cudaError_t launch_paged_umma(PagedAttnArgs a, int hd, cudaStream_t st) {
-  a.groups = (a.hq / a.pool.n_kv_heads * a.c + kQueries - 1) / kQueries;
+  set_groups(a, kQueries);
   a.status = (unsigned int *)a.parts;
   a.parts = (float *)((char *)a.parts + status_bytes());
   PageMaps maps;

@@ -221,18 +221,17 @@ void key_tiles(int len, int rows, int cap, int w, int s, int keys, int *out) {
   out[0] = t.n;
   for (int i = 0; i < t.n && i < 4000; ++i) out[1 + i] = fc::tile_key(t, i, keys);
 }
-long long chunk_of(long long total, int n) { return fc::chunk_of(total, n); }
-void unit_parts(long long begin, int n, long long chunk, int *out) { const fc::UnitParts p = fc::unit_parts(begin, n, chunk); out[0] = p.first; out[1] = p.last; }
-int part_place(long long begin, int worker, long long chunk) { return fc::part_place(begin, worker, chunk); }
+int chunk_of(int total, int n) { return fc::chunk_of(total, n); }
+int quotient16(int x, int n) { return fc::quotient16(x, fc::reciprocal16(n)); }
+int line_batch(int u, int cap, int k) { return fc::line_batch(u, cap, k); }
+int line_fits(int nq, int hkv, int hd, int f32, int cap) { return fc::paged_line_fits(nq, hkv, hd, f32 != 0, cap); }
+void unit_parts(int begin, int n, int chunk, int *out) { const fc::UnitParts p = fc::unit_parts(begin, n, chunk); out[0] = p.first; out[1] = p.last; }
+int part_place(int begin, int worker, int chunk) { return fc::part_place(begin, worker, chunk); }
 int paged_cluster(int b, int u, int cap, int c, int w, int s, int keys, int warps, int sms) { return fc::paged_cluster(b, u, cap, c, w, s, keys, warps, sms); }
 }
 """)
     subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", build.CSRC, "-I", build.INCLUDE, str(src), "-o", str(so)])
     lib_ = C.CDLL(str(so))
-    lib_.chunk_of.restype = C.c_longlong
-    lib_.chunk_of.argtypes = [C.c_longlong, C.c_int]
-    lib_.unit_parts.argtypes = [C.c_longlong, C.c_int, C.c_longlong, C.c_void_p]
-    lib_.part_place.argtypes = [C.c_longlong, C.c_int, C.c_longlong]
     return lib_
 
 
@@ -299,6 +298,23 @@ def test_pieces_of_the_line_and_the_parts_of_units(parts):
                 assert not have
             else:
                 assert have == {w: parts.part_place(s, w, chunk) for w in range(out[0], out[1] + 1)}
+
+
+def test_numbers_of_the_line_stay_within_31_bits(parts):
+    for total in (0, 1, 147, 148, 149, 2 ** 31 - 1):
+        chunk = parts.chunk_of(total, 148)
+        assert chunk * 148 >= total and (total == 0 or chunk * 148 - total < 148)
+    for units, cap, keys in ((1, 16, 16), (4096, 2 ** 20, 16), (7, 2 ** 31 - 1024, 8), (2 ** 20, 2 ** 31 - 1024, 8)):
+        n = parts.line_batch(units, cap, keys)
+        most = units * -(-cap // keys)
+        assert n * most < 2 ** 31 and (n == 0) == (units * (cap // keys + 1) >= 2 ** 31)
+    assert parts.line_fits(16, 32, 128, 0, 2 ** 24) and not parts.line_fits(16, 512, 128, 0, 2 ** 31 - 1024)
+    assert parts.line_fits(1, 32, 128, 1, 2 ** 24) and not parts.line_fits(64, 64, 128, 1, 2 ** 30)
+
+
+def test_queries_are_divided_exactly(parts):
+    for n in list(range(1, 70)) + [128, 255, 512]:
+        assert all(parts.quotient16(x, n) == x // n for x in range(0, 65536, 7 if n > 16 else 1))
 
 
 def test_clusters_only_where_they_all_run_at_once_and_have_little_to_do(parts):
