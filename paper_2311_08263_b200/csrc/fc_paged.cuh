@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
   asm volatile("griddepcontrol.wait;" ::: "memory");
   bool lost = false;                                     // a CTA that gave up a wait left nothing that counts
   if (a.status) {
-    for (int i = w.first; i <= w.last; ++i) lost |= __ldcg(a.status + i) != 0u;
+    lost = __syncthreads_or(tid <= w.last - w.first && __ldcg(a.status + w.first + tid) != 0u);
     if (w.first == w.last && !lost) return;
   }
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;

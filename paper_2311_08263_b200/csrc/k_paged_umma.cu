@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       int i = 0;
       for (int so = 0; i < n_all && ok; ++so) {          // segment by segment
         const int seg_n = min(n_all - i, ld.k.n - ld.t);
-        if (keys && !load_queries(ld, so)) break;
+        if (!keys && !load_queries(ld, so)) break;       // by the warp whose tiles are wanted later
         const int see_from = window_first(ld.len + quotient16(ld.qg * kQueries, a.group_inv), a.window);
         const int see_to = min(ld.len + quotient16(min(nq - 1, ld.qg * kQueries + kQueries - 1), a.group_inv), a.cap - 1);
         for (int g0 = 0; g0 < seg_n && ok; g0 += ahead) {
