@@ -11,7 +11,10 @@ namespace fc {
 
 namespace {
 
-constexpr int kWorkers = 148;          // CTAs on the line: one per SM
+constexpr int kSms = 148;              // CTAs on the line: one per SM
+// How a launch shares its work.  kLine: the line of tiles, a piece per CTA, whose warps take turns at the tiles.  kSolo: a piece per warp, which needs no
+// other warp's results: where there are many units, so that pieces hold whole ones.  kCluster: a cluster per unit.
+enum Mode { kLine, kSolo, kCluster };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -122,11 +125,12 @@ __device__ __forceinline__ uint32_t poff(int r, int ch) {
   return (uint32_t)(ch >> 3) * (KEYS * 128u) + (uint32_t)r * 128u + (uint32_t)(((ch & 7) ^ (r & 7)) << 4);
 }
 
-// A warp's own stream of tiles: every STEP-th tile of a CTA's piece of work into a ring of S stages (keys, then values, of KEYS rows of ROW bytes).
+// A warp's own stream of tiles: those of its piece, or every WARPS-th of its CTA's, into a ring of S stages (keys, then values, of KEYS rows of ROW bytes).
 // The lanes' keys are looked up in the table a tile ahead of the copies, which first use what was read then.
-template <int KEYS, int ROW, int S, int STEP, int QUERIES, bool LINE>
+template <int KEYS, int ROW, int S, int QUERIES, Mode MODE, int WARPS>
 struct TileStream {
   static constexpr uint32_t kHalf = KEYS * ROW, kTile = 2 * kHalf;
+  static constexpr int STEP = MODE == kSolo ? 1 : WARPS;
   static constexpr int PER = ROW / 16, RPI = 32 / PER;   // 16-byte pieces of a row; rows that the lanes load at once
   static constexpr int kUnseen = -2;                     // a key that no query sees; -1: the table has no page for it
   static_assert(KEYS <= 32 && 32 % KEYS == 0 && KEYS % RPI == 0, "lanes, keys and rows");
@@ -142,8 +146,8 @@ struct TileStream {
       : a(args), at(begin), i(first), n(count), page(kUnseen), slot(0), ring(smem), bad_keys(bad) {
     nq = a.nq;
     if (i < n) {
-      if (LINE) move_on<KEYS>(a, at, first);
-      else at.t += first;
+      if (MODE == kLine) move_on<KEYS>(a, at, first);
+      if (MODE == kCluster) at.t += first;
       unit_keys();
       look_up();
     }
@@ -182,7 +186,7 @@ struct TileStream {
       }
       i += STEP;
       if (i < n) {
-        if (LINE) {
+        if (MODE != kCluster) {
           if (move_on<KEYS>(a, at, STEP)) unit_keys();
         } else {
           at.t += STEP;
@@ -194,14 +198,14 @@ struct TileStream {
   }
 };
 
-// What a CTA has to do: the place of its first tile, and how many there are.  LINE: its piece of the line; else its share of one unit (grid: CTAs of the
-// cluster, units, sequences).  False where the line has nothing for it.
-template <int KEYS, bool LINE>
-__device__ __forceinline__ bool my_piece(const PagedAttnArgs &a, Place &seg, int &n) {
-  if (LINE) {
+// What a CTA (kSolo: a warp) has to do: the place of its first tile, and how many there are.  kLine, kSolo: its piece of the line, as one of `workers`;
+// else its share of one unit (grid: CTAs of the cluster, units, sequences).  False where the line has nothing for it.
+template <int KEYS, Mode MODE>
+__device__ __forceinline__ bool my_piece(const PagedAttnArgs &a, int worker, int workers, Place &seg, int &n) {
+  if (MODE != kCluster) {
     int total, unused;
     count_tiles<KEYS>(a, 0, total, unused);
-    const int chunk = chunk_of(total, kWorkers), f0 = chunk * (int)blockIdx.x;       // chunk x workers < 2^31 + workers
+    const int chunk = chunk_of(total, workers), f0 = chunk * worker;       // chunk x workers < 2^31 + workers
     if (f0 >= total || f0 < 0) return false;
     n = min(total - f0, chunk);
     seg = find_place<KEYS>(a, f0);
@@ -257,7 +261,7 @@ __device__ __forceinline__ void join_cluster(const PagedAttnArgs &a, const Place
 constexpr int kCombine = 256;
 
 template <int HD, int Q, int KEYS>
-__global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_constant__ PagedAttnArgs a, int block_rows) {
+__global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_constant__ PagedAttnArgs a, int workers, int block_rows) {
   __shared__ int counts[2];
   __shared__ float4 acc_s[kCombine];
   __shared__ float2 ml_s[kCombine];
@@ -274,11 +278,11 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
   const int kvh = u / a.groups, q0 = (u - kvh * a.groups) * Q, row0 = blockIdx.y * block_rows;
   const int n_rows = min(block_rows, min(Q, nq - q0) - row0), items = n_rows * (HD / 4);
   if (n_rows <= 0) return;
-  const int chunk = chunk_of(counts[0], kWorkers), begin = counts[1] + u * k.n;
+  const int chunk = chunk_of(counts[0], workers), begin = counts[1] + u * k.n;
   UnitParts w = {0, -1};
   if (k.n > 0) {
     w = unit_parts(begin, k.n, chunk);
-    if (w.first == w.last && !a.status) return;          // written by its one CTA
+    if (w.first == w.last && !a.status) return;          // written by its one worker
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   bool lost = false;                                     // a CTA that gave up a wait left nothing that counts
@@ -353,10 +357,10 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
 
 // Blocks of the launch behind the line: whole units, or fewer queries per block while there are not enough blocks for the GPU.
 template <int HD, int Q, int KEYS>
-cudaError_t launch_combine(const PagedAttnArgs &a, cudaStream_t st) {
+cudaError_t launch_combine(const PagedAttnArgs &a, int workers, cudaStream_t st) {
   const long long units = (long long)a.batch * a.groups * a.pool.n_kv_heads;
   int rows = Q < 16 ? Q : 16;
-  while (rows > 1 && units * (Q / rows) < kWorkers) rows /= 2;
+  while (rows > 1 && units * (Q / rows) < kSms) rows /= 2;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = dim3((unsigned)units, Q / rows); cfg.blockDim = dim3(kCombine); cfg.stream = st;
@@ -364,7 +368,7 @@ cudaError_t launch_combine(const PagedAttnArgs &a, cudaStream_t st) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, paged_combine_kernel<HD, Q, KEYS>, a, rows);
+  return cudaLaunchKernelEx(&cfg, paged_combine_kernel<HD, Q, KEYS>, a, workers, rows);
 }
 template <typename K>
 cudaError_t allow_smem(K kernel, size_t bytes, bool *done) {
@@ -399,23 +403,26 @@ cudaError_t by_lines(const PagedAttnArgs &all, int keys, F launch) {
   return cudaSuccess;
 }
 
-// The line and the kernel that joins its parts, or clusters where paged_cluster says so.
-template <int HD, int Q, int KEYS, typename L, typename C>
-cudaError_t launch_units(PagedAttnArgs a, L line, C cluster, int warps, size_t smem, bool *line_done, bool *cluster_done, cudaStream_t st) {
+// The line and the kernel that joins its parts, by CTAs or by warps, or clusters.
+// By warps from two units per SM on.
+template <int HD, int Q, int KEYS, typename K>
+cudaError_t launch_units(PagedAttnArgs a, K line, K solo, K cluster, int warps, size_t smem, bool (*done)[kMaxDevices], cudaStream_t st) {
   set_groups(a, Q);
-  const int ctas = paged_cluster(a.batch, a.groups * a.pool.n_kv_heads, a.cap, a.c, a.window, a.n_sink, KEYS, warps, kWorkers);
+  const int units = a.groups * a.pool.n_kv_heads;
+  const int ctas = paged_cluster(a.batch, units, a.cap, a.c, a.window, a.n_sink, KEYS, warps, kSms);
   if (ctas == 0) {
-    if (cudaError_t e = allow_smem(line, smem, line_done)) return e;
+    const bool by_warps = paged_solo(a.batch, units, kSms);
+    if (cudaError_t e = allow_smem(by_warps ? solo : line, smem, done[by_warps])) return e;
     return by_lines(a, KEYS, [&](const PagedAttnArgs &part) {
-      line<<<kWorkers, warps * 32, smem, st>>>(part);
+      (by_warps ? solo : line)<<<kSms, warps * 32, smem, st>>>(part);
       if (cudaError_t e = cudaGetLastError()) return e;
-      return launch_combine<HD, Q, KEYS>(part, st);
+      return launch_combine<HD, Q, KEYS>(part, by_warps ? kSms * warps : kSms, st);
     });
   }
-  if (cudaError_t e = allow_smem(cluster, smem, cluster_done)) return e;
+  if (cudaError_t e = allow_smem(cluster, smem, done[2])) return e;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
-  cfg.gridDim = dim3(ctas, a.groups * a.pool.n_kv_heads, a.batch); cfg.blockDim = dim3(warps * 32); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.gridDim = dim3(ctas, units, a.batch); cfg.blockDim = dim3(warps * 32); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;

@@ -41,13 +41,13 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   return r;
 }
 // QN: blocks of 8 queries of a unit.  LINE: the line of tiles, else a cluster per unit (grid: CTAs of the cluster, units, sequences).
-template <int HD, int QN, bool LINE>
+template <int HD, int QN, Mode MODE>
 __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_constant__ PagedAttnArgs a) {
   using C = PagedCfg<HD>;
   constexpr int W = kWarps, S = C::S, KS = HD / 16, DB = C::DB, Q = 8 * QN;
   constexpr int PER = HD / 8;                            // 16-byte pieces of a row
   constexpr int OWN = (DB + W - 1) / W;                  // blocks of elements that a warp adds up
-  if (LINE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (MODE != kCluster) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
   __shared__ float2 ml[W][Q];                            // (max, sum) per warp and query
   __shared__ unsigned int bad_keys[W][S];                // keys of a tile whose page is missing
@@ -63,13 +63,16 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
   Place seg;                                             // where the segment (a unit's tiles in this CTA's piece) begins
   int n_mine;
-  if (!my_piece<kKeys, LINE>(a, seg, n_mine)) return;
-  TileStream<kKeys, C::kRow, S, W, Q, LINE> stream(a, seg, warp, n_mine, ring, bad_keys[warp]);
+  // a warp that works on its own: consecutive pieces on different SMs
+  const int worker = MODE == kSolo ? warp * kSms + (int)blockIdx.x : (int)blockIdx.x;
+  if (!my_piece<kKeys, MODE>(a, worker, MODE == kSolo ? W * kSms : kSms, seg, n_mine)) return;
+  constexpr int STEP = MODE == kSolo ? 1 : W;
+  TileStream<kKeys, C::kRow, S, Q, MODE, W> stream(a, seg, MODE == kSolo ? 0 : warp, n_mine, ring, bad_keys[warp]);
 #pragma unroll 1
   for (int s = 0; s < S - 1; ++s) stream.request(s);
 
   int stage = 0;
-  int i = warp;                                          // this warp's next tile in the piece
+  int i = MODE == kSolo ? 0 : warp;                      // this warp's next tile in the piece
   int done = 0;                                          // tiles of the piece in front of the segment
   while (true) {
     // ---- a segment: tiles done .. done + seg_n of the piece, tiles seg.t .. of the unit
@@ -106,7 +109,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
         for (int x = 0; x < 4; ++x) o[n][d][x] = 0.f;
     }
 
-    for (; i < done + seg_n; i += W) {
+    for (; i < done + seg_n; i += STEP) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
       __syncwarp();                                      // everybody's copies are here, and the stage before is free
       stream.request(stage == 0 ? S - 1 : stage - 1);
@@ -251,12 +254,36 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
         l_run[n][x] += __shfl_xor_sync(0xffffffffu, l_run[n][x], 4);
         l_run[n][x] += __shfl_xor_sync(0xffffffffu, l_run[n][x], 8);
         l_run[n][x] += __shfl_xor_sync(0xffffffffu, l_run[n][x], 16);
-        if (g4 == 0) ml[warp][n * 8 + t4 * 2 + x] = make_float2(m_run[n][x], l_run[n][x]);
+        if (MODE != kSolo && g4 == 0) ml[warp][n * 8 + t4 * 2 + x] = make_float2(m_run[n][x], l_run[n][x]);
       }
-    const bool whole = LINE ? seg_n == seg.k.n : gridDim.x == 1;
+    const bool whole = MODE != kCluster ? seg_n == seg.k.n : gridDim.x == 1;
+    if (MODE == kSolo) {
+      // ---- all of it is this warp's
+      float *part = a.parts + ((long long)worker * 2 + (done > 0)) * part_floats(Q, HD);
+#pragma unroll
+      for (int n = 0; n < QN; ++n)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int q = q0 + n * 8 + t4 * 2 + x;
+          if (q >= nq) continue;
+          const int j = quotient16(q, a.group_inv), h = seg.kvh * group + q - j * group;
+          const float f = whole ? result_scale(a, pos[n][x], l_run[n][x]) : 1.f;
+          float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + (q - q0) * HD;
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            to[d * 16 + g4] = o[n][d][x] * f;
+            to[d * 16 + g4 + 8] = o[n][d][x + 2] * f;
+          }
+          if (!whole && g4 == 0) *reinterpret_cast<float2 *>(part + Q * HD + (q - q0) * 2) = make_float2(m_run[n][x], l_run[n][x]);
+        }
+      done += seg_n;
+      if (done == n_mine) break;
+      move_on<kKeys>(a, seg, seg_n);
+      continue;
+    }
     // where sums go that are not the whole unit's: scratch, or this CTA's shared memory (the ring, drained)
-    float *part = LINE ? a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * part_floats(Q, HD) : reinterpret_cast<float *>(base_g);
-    if (!LINE) {
+    float *part = MODE == kLine ? a.parts + ((long long)worker * 2 + (done > 0)) * part_floats(Q, HD) : reinterpret_cast<float *>(base_g);
+    if (MODE == kCluster) {
       asm volatile("cp.async.wait_all;" ::: "memory");
       __syncthreads();
     }
@@ -307,19 +334,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
           to[d * 16 + g4] = sum[x] * f;
           to[d * 16 + g4 + 8] = sum[x + 2] * f;
           if (!whole && d == 0 && g4 == 0) {
-            if (LINE) *reinterpret_cast<float2 *>(part + Q * HD + (q - q0) * 2) = make_float2(M[x], den[x]);
+            if (MODE == kLine) *reinterpret_cast<float2 *>(part + Q * HD + (q - q0) * 2) = make_float2(M[x], den[x]);
             else ml_cta[q - q0] = make_float2(M[x], den[x]);
           }
         }
       }
     }
-    if (!LINE) break;
+    if (MODE == kCluster) break;
     done += seg_n;
     if (done == n_mine) break;
     move_on<kKeys>(a, seg, seg_n);
     __syncthreads();                                     // the exchange buffers are free again
   }
-  if (LINE) {
+  if (MODE != kCluster) {
     asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
@@ -331,8 +358,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
 // ------------------------------------------------------------------------------------ host side
 template <int HD, int QN>
 cudaError_t launch_mma(const PagedAttnArgs &a, cudaStream_t st) {
-  static bool line[kMaxDevices] = {false}, cluster[kMaxDevices] = {false};
-  return launch_units<HD, 8 * QN, kKeys>(a, paged_mma_kernel<HD, QN, true>, paged_mma_kernel<HD, QN, false>, kWarps, PagedCfg<HD>::kSmem, line, cluster, st);
+  static bool done[3][kMaxDevices] = {};
+  return launch_units<HD, 8 * QN, kKeys>(a, paged_mma_kernel<HD, QN, kLine>, paged_mma_kernel<HD, QN, kSolo>, paged_mma_kernel<HD, QN, kCluster>, kWarps,
+                                         PagedCfg<HD>::kSmem, done, st);
 }
 template <int HD>
 cudaError_t launch_hd(const PagedAttnArgs &a, cudaStream_t st) {
@@ -345,7 +373,7 @@ cudaError_t launch_hd(const PagedAttnArgs &a, cudaStream_t st) {
 
 size_t paged_attn_scratch(int nq, int hd, int dtype) {
   if (dtype == FC_F32) return paged_fma_scratch(hd);
-  return paged_umma(nq, hd) ? paged_umma_scratch(hd) : (size_t)kWorkers * 2 * part_floats(16, hd) * sizeof(float);
+  return paged_umma(nq, hd) ? paged_umma_scratch(hd) : (size_t)kSms * kWarps * 2 * part_floats(16, hd) * sizeof(float);
 }
 
 cudaError_t launch_paged_attn(PagedAttnArgs a, int dtype, int hd, cudaStream_t st) {

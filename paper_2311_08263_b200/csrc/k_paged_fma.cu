@@ -20,14 +20,14 @@ struct FmaCfg {
   static constexpr uint32_t kP = kWarps * KEYS * QB * 4;            // probabilities, per warp [key][query]
   static constexpr int XQ = QB < 4 ? QB : 4;                        // queries that are exchanged at a time
   static constexpr uint32_t kExchange = kWarps * XQ * HD * 4;
-  static constexpr size_t kSmem = 128 + kRing + kQ + kP + kExchange;
+  static constexpr size_t kSmem = 128 + kRing + kP + (kQ + kExchange > kWarps * kQ ? kQ + kExchange : kWarps * kQ);
 };
 
-template <int HD, int QB, bool LINE>
+template <int HD, int QB, Mode MODE>
 __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_constant__ PagedAttnArgs a) {
   using C = FmaCfg<HD, QB>;
   constexpr int W = kWarps, S = C::S, KEYS = C::KEYS, PARTS = 32 / KEYS, E = HD / 32;
-  if (LINE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (MODE != kCluster) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
   __shared__ float2 ml[W][QB], ml_cta[QB];               // (max, sum)
   __shared__ unsigned int bad_keys[W][S];
@@ -36,30 +36,37 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
   const uint32_t base = (smem_u32(smem_raw) + 127u) & ~127u;
   unsigned char *base_g = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t ring = base + (uint32_t)warp * (S * C::kTile);
-  float *qs = reinterpret_cast<float *>(base_g + C::kRing);
-  float *ps = qs + QB * HD + warp * KEYS * QB;
-  float *exchange = qs + QB * HD + W * KEYS * QB;
+  float *ps = reinterpret_cast<float *>(base_g + C::kRing) + warp * KEYS * QB;
+  // the unit's queries, and room for the exchange; a warp on its own has its queries where the others would exchange
+  float *qs = reinterpret_cast<float *>(base_g + C::kRing + C::kP) + (MODE == kSolo ? warp * QB * HD : 0);
+  float *exchange = reinterpret_cast<float *>(base_g + C::kRing + C::kP + C::kQ);
 
   const int group = a.group, nq = a.nq;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
   Place seg;
   int n_mine;
-  if (!my_piece<KEYS, LINE>(a, seg, n_mine)) return;
-  TileStream<KEYS, C::kRow, S, W, QB, LINE> stream(a, seg, warp, n_mine, ring, bad_keys[warp]);
+  // a warp that works on its own: consecutive pieces on different SMs
+  const int worker = MODE == kSolo ? warp * kSms + (int)blockIdx.x : (int)blockIdx.x;
+  if (!my_piece<KEYS, MODE>(a, worker, MODE == kSolo ? W * kSms : kSms, seg, n_mine)) return;
+  constexpr int STEP = MODE == kSolo ? 1 : W;
+  TileStream<KEYS, C::kRow, S, QB, MODE, W> stream(a, seg, MODE == kSolo ? 0 : warp, n_mine, ring, bad_keys[warp]);
 #pragma unroll 1
   for (int s = 0; s < S - 1; ++s) stream.request(s);
 
   const int key = lane % KEYS, share = lane / KEYS;      // a lane's key, and which 32 elements of it
-  int stage = 0, i = warp, done = 0;
+  int stage = 0, i = MODE == kSolo ? 0 : warp, done = 0;
   while (true) {
     // ---- a segment: tiles done .. done + seg_n of the piece, tiles seg.t .. of the unit
     const int seg_n = min(n_mine - done, seg.k.n - seg.t);
     const int q0 = seg.qg * QB, q_last = min(nq - 1, q0 + QB - 1);
-    for (int e = tid; e < QB * (HD / 4); e += kThreads) {
+    // kSolo: the warps have places of their own for the queries
+    if (MODE == kSolo) __syncwarp();
+    for (int e = MODE == kSolo ? lane : tid; e < QB * (HD / 4); e += MODE == kSolo ? 32 : kThreads) {
       const int n = e / (HD / 4), c4 = e - n * (HD / 4), q = min(q0 + n, nq - 1), j = quotient16(q, a.group_inv), h = seg.kvh * group + q - j * group;
       reinterpret_cast<float4 *>(qs)[e] = *reinterpret_cast<const float4 *>((const float *)a.q + ((long long)seg.b * a.c + j) * a.q_stride + h * HD + c4 * 4);
     }
-    __syncthreads();
+    if (MODE == kSolo) __syncwarp();
+    else __syncthreads();
     int pos[QB];
     float m[QB], l[QB], o[QB][E];
 #pragma unroll
@@ -72,7 +79,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
     }
     const int p_first = seg.len + quotient16(q0, a.group_inv), p_last = seg.len + quotient16(q_last, a.group_inv), low_last = window_first(p_last, a.window);
 
-    for (; i < done + seg_n; i += W) {
+    for (; i < done + seg_n; i += STEP) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
       __syncwarp();                                      // everybody's copies are here, and the stage before is free
       stream.request(stage == 0 ? S - 1 : stage - 1);
@@ -176,12 +183,31 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
     for (int n = 0; n < QB; ++n) {
 #pragma unroll
       for (int d = 1; d < KEYS; d <<= 1) l[n] += __shfl_xor_sync(0xffffffffu, l[n], d);
-      if (lane == 0) ml[warp][n] = make_float2(m[n], l[n]);
+      if (MODE != kSolo && lane == 0) ml[warp][n] = make_float2(m[n], l[n]);
     }
-    if (!LINE) asm volatile("cp.async.wait_all;" ::: "memory");
-    const bool whole = LINE ? seg_n == seg.k.n : gridDim.x == 1;
+    if (MODE == kCluster) asm volatile("cp.async.wait_all;" ::: "memory");
+    const bool whole = MODE != kCluster ? seg_n == seg.k.n : gridDim.x == 1;
+    if (MODE == kSolo) {
+      // ---- all of it is this warp's
+      float *part = a.parts + ((long long)worker * 2 + (done > 0)) * part_floats(QB, HD);
+#pragma unroll
+      for (int n = 0; n < QB; ++n) {
+        const int q = q0 + n;
+        if (q >= nq) continue;
+        const int j = quotient16(q, a.group_inv), h = seg.kvh * group + q - j * group;
+        const float f = whole ? result_scale(a, pos[n], l[n]) : 1.f;
+        float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + n * HD;
+#pragma unroll
+        for (int e = 0; e < E; ++e) to[lane * E + e] = o[n][e] * f;
+        if (!whole && lane == 0) *reinterpret_cast<float2 *>(part + QB * HD + n * 2) = make_float2(m[n], l[n]);
+      }
+      done += seg_n;
+      if (done == n_mine) break;
+      move_on<KEYS>(a, seg, seg_n);
+      continue;
+    }
     // sums that are not the whole unit's: scratch, or this CTA's shared memory (the ring, drained)
-    float *part = LINE ? a.parts + ((long long)blockIdx.x * 2 + (done > 0)) * part_floats(QB, HD) : reinterpret_cast<float *>(base_g);
+    float *part = MODE == kLine ? a.parts + ((long long)worker * 2 + (done > 0)) * part_floats(QB, HD) : reinterpret_cast<float *>(base_g);
 #pragma unroll
     for (int n0 = 0; n0 < QB; n0 += C::XQ) {
       if (n0) __syncthreads();
@@ -208,18 +234,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
         float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + n * HD;
         *reinterpret_cast<float4 *>(to + c4 * 4) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
         if (!whole && c4 == 0) {
-          if (LINE) *reinterpret_cast<float2 *>(part + QB * HD + n * 2) = make_float2(M, den);
+          if (MODE == kLine) *reinterpret_cast<float2 *>(part + QB * HD + n * 2) = make_float2(M, den);
           else ml_cta[n] = make_float2(M, den);
         }
       }
     }
-    if (!LINE) break;
+    if (MODE == kCluster) break;
     done += seg_n;
     if (done == n_mine) break;
     move_on<KEYS>(a, seg, seg_n);
     __syncthreads();                                     // the queries and the exchange are free again
   }
-  if (LINE) {
+  if (MODE != kCluster) {
     asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
@@ -231,8 +257,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
 template <int HD, int QB>
 cudaError_t launch(const PagedAttnArgs &a, cudaStream_t st) {
   using C = FmaCfg<HD, QB>;
-  static bool line[kMaxDevices] = {false}, cluster[kMaxDevices] = {false};
-  return launch_units<HD, QB, C::KEYS>(a, paged_fma_kernel<HD, QB, true>, paged_fma_kernel<HD, QB, false>, kWarps, C::kSmem, line, cluster, st);
+  static bool done[3][kMaxDevices] = {};
+  return launch_units<HD, QB, C::KEYS>(a, paged_fma_kernel<HD, QB, kLine>, paged_fma_kernel<HD, QB, kSolo>, paged_fma_kernel<HD, QB, kCluster>, kWarps, C::kSmem,
+                                       done, st);
 }
 template <int HD>
 cudaError_t launch_hd(const PagedAttnArgs &a, cudaStream_t st) {
@@ -241,7 +268,7 @@ cudaError_t launch_hd(const PagedAttnArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-size_t paged_fma_scratch(int hd) { return (size_t)kWorkers * 2 * part_floats(8, hd) * sizeof(float); }
+size_t paged_fma_scratch(int hd) { return (size_t)kSms * kWarps * 2 * part_floats(8, hd) * sizeof(float); }
 
 cudaError_t launch_paged_fma(const PagedAttnArgs &a, int hd, cudaStream_t st) {
   return hd == 128 ? launch_hd<128>(a, st) : hd == 64 ? launch_hd<64>(a, st) : launch_hd<32>(a, st);

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
 
   Place seg;
   int n_mine;
-  if (!my_piece<kKeys, true>(a, seg, n_mine)) return;
+  if (!my_piece<kKeys, kLine>(a, blockIdx.x, kSms, seg, n_mine)) return;
 
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
@@ -660,17 +660,17 @@ cudaError_t launch(const PageMaps &maps, const PagedAttnArgs &a, cudaStream_t st
     if (cudaError_t e = allow_smem(paged_umma_kernel<HD, TMA>, C::kSmem, done)) return e;
   }
   return by_lines(a, kKeys, [&](const PagedAttnArgs &part) {
-    paged_umma_kernel<HD, TMA><<<kWorkers, kThreads, C::kSmem, st>>>(maps, part);
+    paged_umma_kernel<HD, TMA><<<kSms, kThreads, C::kSmem, st>>>(maps, part);
     if (cudaError_t e = cudaGetLastError()) return e;
-    return launch_combine<HD, kQueries, kKeys>(part, st);
+    return launch_combine<HD, kQueries, kKeys>(part, kSms, st);
   });
 }
 
-size_t status_bytes() { return (kWorkers * sizeof(unsigned int) + 255) / 256 * 256; }
+size_t status_bytes() { return (kSms * sizeof(unsigned int) + 255) / 256 * 256; }
 
 }  // namespace
 
-size_t paged_umma_scratch(int hd) { return status_bytes() + (size_t)kWorkers * 2 * part_floats(kQueries, hd) * sizeof(float); }
+size_t paged_umma_scratch(int hd) { return status_bytes() + (size_t)kSms * 2 * part_floats(kQueries, hd) * sizeof(float); }
 
 cudaError_t launch_paged_umma(PagedAttnArgs a, int hd, cudaStream_t st) {
   set_groups(a, kQueries);

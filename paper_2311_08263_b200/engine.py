@@ -6,6 +6,7 @@ CUDA library.  Method names match the C entry points they call.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import Dict, Optional
 
 import numpy as np
@@ -301,44 +302,50 @@ def fc_op_short_window_attention(qkv_acc: torch.Tensor, sumsq: torch.Tensor, rms
 _CACHE_TYPES = {torch.float32: _l.FC_F32, torch.bfloat16: _l.FC_BF16}
 _POOL = ("k and v: fp32 or bf16 tensors of the same shape and strides on one CUDA device, adjacent elements, "
          "[layers, pages, kv heads, slots, head size] (operations on one layer: without the first dimension)")
+_raw_stream = torch._C._cuda_getCurrentRawStream        # a stream object costs two microseconds
 
 
+# What these calls cost is mostly what Python does for them, so each looks at a tensor's properties once and by the cheapest accessor.
 def _pool(k: torch.Tensor, v: torch.Tensor, dims: int) -> _l.fc_pages:
     shape, stride, dtype = k.shape, k.stride(), _CACHE_TYPES.get(k.dtype)
     if (dtype is None or len(shape) != dims or v.shape != shape or v.stride() != stride or v.dtype is not k.dtype or stride[-1] != 1
-            or not k.is_cuda or v.device != k.device):
+            or k.get_device() < 0 or v.get_device() != k.get_device()):
         raise ValueError(_POOL)
     if dims == 4:
-        return _l.fc_pages(k.data_ptr(), v.data_ptr(), dtype, 1, *shape, 0, stride[0], stride[1], stride[2])
+        return _l.fc_pages(k.data_ptr(), v.data_ptr(), dtype, 1, *shape, 0, *stride[:3])
     return _l.fc_pages(k.data_ptr(), v.data_ptr(), dtype, *shape, *stride[:4])
 
 
-def _ints(name: str, t: torch.Tensor, dims: int, dev) -> int:
-    if t.dtype is not torch.int32 or t.dim() != dims or not t.is_contiguous() or t.device != dev or not t.is_cuda:
+def _ints(name: str, t: torch.Tensor, dims: int, device: int) -> int:
+    if t.dtype is not torch.int32 or t.dim() != dims or not t.is_contiguous() or t.get_device() != device or device < 0:
         raise ValueError(f"{name}: contiguous int32 tensor of {dims} dimension(s) on the pool's CUDA device")
     return t.data_ptr()
 
 
-def _lengths(kv_len: torch.Tensor, table: torch.Tensor, dev) -> int:
-    if kv_len.shape[0] != table.shape[0]:
+def _lengths(kv_len: torch.Tensor, n: int, device: int) -> int:
+    if kv_len.numel() != n:
         raise ValueError("kv_len: one length per row of the table")
-    return _ints("kv_len", kv_len, 1, dev)
+    return _ints("kv_len", kv_len, 1, device)
 
 
 def _list(ids):
     return (C.c_int32 * len(ids))(*ids)
 
 
-def _enqueue(dev, where: str, fn, *args):
-    """The call on the device's current stream (by its number: the stream object costs two microseconds)."""
-    at = dev.index
-    if at == torch.cuda.current_device():
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(at))
+def _enqueue(device: int, fn, *args) -> None:
+    """The call on the current stream of the tensors' device."""
+    if device == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(device))
     else:
-        with torch.cuda.device(at):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(at))
-    if rc != _l.FC_OK:
-        raise FcError(rc, where)
+        with torch.cuda.device(device):
+            rc = fn(*args, _raw_stream(device))
+    if rc:
+        raise FcError(rc, fn.__name__)
+
+
+@functools.lru_cache(maxsize=1024)
+def _scratch_bytes(name: str, *sizes: int) -> int:
+    return getattr(_l.load(), name)(*sizes)
 
 
 def fc_op_paged_store(qkv: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, c: int, n_heads: int,
@@ -346,16 +353,16 @@ def fc_op_paged_store(qkv: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table
     """QKV rows of one layer into pages.  qkv fp32 [B*c, (n_heads + 2 n_kv_heads) * hd], rows adjacent or not; k/v [pages, n_kv_heads,
     slots, hd]; table int32 [B, width]; kv_len int32 [B].  Returns the rotated queries [B*c, n_heads * hd] in the pool's type; those of
     table rows without a sequence are not written."""
-    pool, dev = _pool(k, v, 4), k.device
-    tab = _ints("table", table, 2, dev)
+    pool, device = _pool(k, v, 4), k.get_device()
+    tab = _ints("table", table, 2, device)
     B, width = table.shape
-    hd = pool.head_dim
-    if (qkv.dtype is not torch.float32 or qkv.shape != (B * c, (n_heads + 2 * pool.n_kv_heads) * hd) or qkv.stride(1) != 1
-            or qkv.device != dev):
+    row, elem = qkv.stride()
+    if (qkv.dtype is not torch.float32 or qkv.shape != (B * c, (n_heads + 2 * pool.n_kv_heads) * pool.head_dim) or elem != 1
+            or qkv.get_device() != device):
         raise ValueError("qkv: fp32 [B * c, (n_heads + 2 n_kv_heads) * head size] with adjacent elements, on the pool's device")
-    q = torch.empty(B * c, n_heads * hd, dtype=k.dtype, device=dev)
-    _enqueue(dev, "fc_op_paged_store", _l.load().fc_op_paged_store, pool, 0, tab, width, _lengths(kv_len, table, dev), qkv.data_ptr(),
-             qkv.stride(0), q.data_ptr(), B, c, n_heads, rope_theta)
+    q = torch.empty(B * c, n_heads * pool.head_dim, dtype=k.dtype, device=k.device)
+    _enqueue(device, _l.load().fc_op_paged_store, pool, 0, tab, width, _lengths(kv_len, B, device), qkv.data_ptr(), row, q.data_ptr(), B, c,
+             n_heads, rope_theta)
     return q
 
 
@@ -363,66 +370,64 @@ def fc_op_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tab
                           n_heads: int, window: int = 0, n_sink: int = 0) -> torch.Tensor:
     """Window attention of one layer over pages, optionally under a sliding window with sinks.  q [B*c, n_heads * hd] in the pool's type,
     rows adjacent or not; the rest as in fc_op_paged_store, the rows' own keys and values stored.  Returns fp32 [B*c, n_heads * hd]."""
-    pool, dev = _pool(k, v, 4), k.device
-    tab = _ints("table", table, 2, dev)
+    pool, device = _pool(k, v, 4), k.get_device()
+    tab = _ints("table", table, 2, device)
     B, width = table.shape
     hd = pool.head_dim
-    if q.dtype is not k.dtype or q.shape != (B * c, n_heads * hd) or q.stride(1) != 1 or q.device != dev:
+    row, elem = q.stride()
+    if q.dtype is not k.dtype or q.shape != (B * c, n_heads * hd) or elem != 1 or q.get_device() != device:
         raise ValueError("q: [B * c, n_heads * head size] in the pool's type with adjacent elements, on the pool's device")
-    lib = _l.load()
-    nbytes = lib.fc_op_paged_attention_scratch_bytes(B, c, n_heads, pool.n_kv_heads, hd, pool.dtype)
-    scratch = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    out = torch.empty(B * c, n_heads * hd, dtype=torch.float32, device=dev)
-    _enqueue(dev, "fc_op_paged_attention", lib.fc_op_paged_attention, pool, 0, tab, width, _lengths(kv_len, table, dev), q.data_ptr(),
-             q.stride(0), out.data_ptr(), B, c, n_heads, window, n_sink, scratch.data_ptr(), nbytes)
+    nbytes = _scratch_bytes("fc_op_paged_attention_scratch_bytes", B, c, n_heads, pool.n_kv_heads, hd, pool.dtype)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=k.device)
+    out = torch.empty(B * c, n_heads * hd, dtype=torch.float32, device=k.device)
+    _enqueue(device, _l.load().fc_op_paged_attention, pool, 0, tab, width, _lengths(kv_len, B, device), q.data_ptr(), row, out.data_ptr(), B, c,
+             n_heads, window, n_sink, scratch.data_ptr(), nbytes)
     return out
 
 
 def fc_op_pages_fork(table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, page_size: int, src, dst) -> None:
     """Table rows dst[i] share the pages of rows src[i]'s committed tokens (lists of row numbers on the host)."""
-    dev, n = table.device, len(dst)
+    device, (rows, width), n = table.get_device(), table.shape, len(dst)
     if len(src) != n:
         raise ValueError("src and dst: two lists of the same length")
-    _enqueue(dev, "fc_op_pages_fork", _l.load().fc_op_pages_fork, _ints("table", table, 2, dev), table.shape[1], table.shape[0],
-             _lengths(kv_len, table, dev), _ints("refs", refs, 1, dev), refs.shape[0], page_size, _list(src), _list(dst), n)
+    _enqueue(device, _l.load().fc_op_pages_fork, _ints("table", table, 2, device), width, rows, _lengths(kv_len, rows, device),
+             _ints("refs", refs, 1, device), refs.numel(), page_size, _list(src), _list(dst), n)
 
 
 def fc_op_pages_free(table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, page_size: int, seqs, window: int = 0,
                      n_sink: int = 0) -> None:
     """Release the pages of table rows `seqs` (a list on the host): all of them, or those that no later row of a sliding window sees."""
-    dev = table.device
-    _enqueue(dev, "fc_op_pages_free", _l.load().fc_op_pages_free, _ints("table", table, 2, dev), table.shape[1], table.shape[0],
-             _lengths(kv_len, table, dev), _ints("refs", refs, 1, dev), refs.shape[0], page_size, _list(seqs), len(seqs), window, n_sink)
+    device, (rows, width) = table.get_device(), table.shape
+    _enqueue(device, _l.load().fc_op_pages_free, _ints("table", table, 2, device), width, rows, _lengths(kv_len, rows, device),
+             _ints("refs", refs, 1, device), refs.numel(), page_size, _list(seqs), len(seqs), window, n_sink)
 
 
 def fc_op_pages_reserve(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor,
                         rows: int) -> torch.Tensor:
     """Pages for positions kv_len .. kv_len + rows - 1 of every sequence, copies of shared ones.  k/v [layers, pages, n_kv_heads, slots, hd].
     Returns int32 [n_seqs]: 1 where the positions can be written."""
-    pool, dev = _pool(k, v, 5), k.device
-    tab, counts = _ints("table", table, 2, dev), _ints("refs", refs, 1, dev)
+    pool, device = _pool(k, v, 5), k.get_device()
+    tab, counts = _ints("table", table, 2, device), _ints("refs", refs, 1, device)
     n, width = table.shape
-    if refs.shape[0] != pool.n_pages:
+    if refs.numel() != pool.n_pages:
         raise ValueError("refs: one count per page")
-    lib = _l.load()
-    nbytes = lib.fc_op_pages_reserve_scratch_bytes(pool.n_pages, n)
-    scratch = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    served = torch.empty(n, dtype=torch.int32, device=dev)
-    _enqueue(dev, "fc_op_pages_reserve", lib.fc_op_pages_reserve, pool, tab, width, n, _lengths(kv_len, table, dev), counts, rows,
-             served.data_ptr(), scratch.data_ptr(), nbytes)
+    nbytes = _scratch_bytes("fc_op_pages_reserve_scratch_bytes", pool.n_pages, n)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=k.device)
+    served = torch.empty(n, dtype=torch.int32, device=k.device)
+    _enqueue(device, _l.load().fc_op_pages_reserve, pool, tab, width, n, _lengths(kv_len, n, device), counts, rows, served.data_ptr(),
+             scratch.data_ptr(), nbytes)
     return served
 
 
 def fc_op_pages_compact(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, refs: torch.Tensor) -> torch.Tensor:
     """Move the pages in use to the front of the pool, in all layers; table and refs follow.  Returns int32 [1]: how many are in use."""
-    pool, dev = _pool(k, v, 5), k.device
-    tab, counts = _ints("table", table, 2, dev), _ints("refs", refs, 1, dev)
-    if refs.shape[0] != pool.n_pages:
+    pool, device = _pool(k, v, 5), k.get_device()
+    tab, counts = _ints("table", table, 2, device), _ints("refs", refs, 1, device)
+    n, width = table.shape
+    if refs.numel() != pool.n_pages:
         raise ValueError("refs: one count per page")
-    lib = _l.load()
-    nbytes = lib.fc_op_pages_compact_scratch_bytes(pool.n_pages)
-    scratch = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    n_live = torch.empty(1, dtype=torch.int32, device=dev)
-    _enqueue(dev, "fc_op_pages_compact", lib.fc_op_pages_compact, pool, tab, table.shape[1], table.shape[0], counts, n_live.data_ptr(),
-             scratch.data_ptr(), nbytes)
+    nbytes = _scratch_bytes("fc_op_pages_compact_scratch_bytes", pool.n_pages)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=k.device)
+    n_live = torch.empty(1, dtype=torch.int32, device=k.device)
+    _enqueue(device, _l.load().fc_op_pages_compact, pool, tab, width, n, counts, n_live.data_ptr(), scratch.data_ptr(), nbytes)
     return n_live
