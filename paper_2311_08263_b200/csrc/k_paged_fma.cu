@@ -26,7 +26,7 @@ struct FmaCfg {
 template <int HD, int QB, Mode MODE>
 __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_constant__ PagedAttnArgs a) {
   using C = FmaCfg<HD, QB>;
-  constexpr int W = kWarps, S = C::S, KEYS = C::KEYS, PARTS = 32 / KEYS, E = HD / 32;
+  constexpr int W = kWarps, S = C::S, KEYS = C::KEYS, E = HD / 32;
   if (MODE != kCluster) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
   __shared__ float2 ml[W][QB], ml_cta[QB];               // (max, sum)
