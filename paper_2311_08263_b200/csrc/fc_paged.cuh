@@ -12,9 +12,6 @@ namespace fc {
 namespace {
 
 constexpr int kSms = 148;              // CTAs on the line: one per SM
-// How a launch shares its work.  kLine: the line of tiles, a piece per CTA, whose warps take turns at the tiles.  kSolo: a piece per warp, which needs no
-// other warp's results: where there are many units, so that pieces hold whole ones.  kCluster: a cluster per unit.
-enum Mode { kLine, kSolo, kCluster };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -125,12 +122,12 @@ __device__ __forceinline__ uint32_t poff(int r, int ch) {
   return (uint32_t)(ch >> 3) * (KEYS * 128u) + (uint32_t)r * 128u + (uint32_t)(((ch & 7) ^ (r & 7)) << 4);
 }
 
-// A warp's own stream of tiles: those of its piece, or every WARPS-th of its CTA's, into a ring of S stages (keys, then values, of KEYS rows of ROW bytes).
+// A warp's own stream of tiles: those of its piece of the line, or every WARPS-th of its CTA's in a cluster, into a ring of S stages (keys, then values, of KEYS rows of ROW bytes).
 // The lanes' keys are looked up in the table a tile ahead of the copies, which first use what was read then.
-template <int KEYS, int ROW, int S, int QUERIES, Mode MODE, int WARPS>
+template <int KEYS, int ROW, int S, int QUERIES, bool LINE, int WARPS>
 struct TileStream {
   static constexpr uint32_t kHalf = KEYS * ROW, kTile = 2 * kHalf;
-  static constexpr int STEP = MODE == kSolo ? 1 : WARPS;
+  static constexpr int STEP = LINE ? 1 : WARPS;
   static constexpr int PER = ROW / 16, RPI = 32 / PER;   // 16-byte pieces of a row; rows that the lanes load at once
   static constexpr int kUnseen = -2;                     // a key that no query sees; -1: the table has no page for it
   static_assert(KEYS <= 32 && 32 % KEYS == 0 && KEYS % RPI == 0, "lanes, keys and rows");
@@ -146,8 +143,7 @@ struct TileStream {
       : a(args), at(begin), i(first), n(count), page(kUnseen), slot(0), ring(smem), bad_keys(bad) {
     nq = a.nq;
     if (i < n) {
-      if (MODE == kLine) move_on<KEYS>(a, at, first);
-      if (MODE == kCluster) at.t += first;
+      at.t += first;                                     // in a cluster: tiles of one unit
       unit_keys();
       look_up();
     }
@@ -186,7 +182,7 @@ struct TileStream {
       }
       i += STEP;
       if (i < n) {
-        if (MODE != kCluster) {
+        if (LINE) {
           if (move_on<KEYS>(a, at, STEP)) unit_keys();
         } else {
           at.t += STEP;
@@ -198,11 +194,11 @@ struct TileStream {
   }
 };
 
-// What a CTA (kSolo: a warp) has to do: the place of its first tile, and how many there are.  kLine, kSolo: its piece of the line, as one of `workers`;
-// else its share of one unit (grid: CTAs of the cluster, units, sequences).  False where the line has nothing for it.
-template <int KEYS, Mode MODE>
+// What there is to do: the place of the first tile, and how many.  LINE: a worker's piece of the line; else a CTA's share of one unit (grid: CTAs of the
+// cluster, units, sequences).  False where the line has nothing for the worker.
+template <int KEYS, bool LINE>
 __device__ __forceinline__ bool my_piece(const PagedAttnArgs &a, int worker, int workers, Place &seg, int &n) {
-  if (MODE != kCluster) {
+  if (LINE) {
     int total, unused;
     count_tiles<KEYS>(a, 0, total, unused);
     const int chunk = chunk_of(total, workers), f0 = chunk * worker;       // chunk x workers < 2^31 + workers
@@ -258,9 +254,10 @@ __device__ __forceinline__ void join_cluster(const PagedAttnArgs &a, const Place
 // ------------------------------------------------------------------------------------ joining the parts of a unit
 // A block takes block_rows queries of a unit: with items = queries x hd / 4 pieces of four elements, threads are groups that take turns at the
 // parts.  A few units have many parts each (one sequence, four kv heads: 37), and then a query per block reads them all at once.
-constexpr int kCombine = 256;
 
-template <int HD, int Q, int KEYS>
+constexpr int kCombine = 256;
+// U: parts that a thread has on their way at once.
+template <int HD, int Q, int KEYS, int U>
 __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_constant__ PagedAttnArgs a, int workers, int block_rows) {
   __shared__ int counts[2];
   __shared__ float4 acc_s[kCombine];
@@ -300,7 +297,6 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
     float m = -INFINITY, den = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (e < items && g < groups) {
-      constexpr int U = 4;
       for (int p = w.first + g; p <= w.last; p += groups * U) {
         float2 v[U];
         float4 x[U];
@@ -368,7 +364,7 @@ cudaError_t launch_combine(const PagedAttnArgs &a, int workers, cudaStream_t st)
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, paged_combine_kernel<HD, Q, KEYS>, a, workers, rows);
+  return cudaLaunchKernelEx(&cfg, rows == 1 ? paged_combine_kernel<HD, Q, KEYS, 8> : paged_combine_kernel<HD, Q, KEYS, 4>, a, workers, rows);
 }
 template <typename K>
 cudaError_t allow_smem(K kernel, size_t bytes, bool *done) {
@@ -403,23 +399,21 @@ cudaError_t by_lines(const PagedAttnArgs &all, int keys, F launch) {
   return cudaSuccess;
 }
 
-// The line and the kernel that joins its parts, by CTAs or by warps, or clusters.
-// By warps from two units per SM on.
+// The line, a piece for every warp, and the kernel that joins its parts; or clusters where paged_cluster says so.
 template <int HD, int Q, int KEYS, typename K>
-cudaError_t launch_units(PagedAttnArgs a, K line, K solo, K cluster, int warps, size_t smem, bool (*done)[kMaxDevices], cudaStream_t st) {
+cudaError_t launch_units(PagedAttnArgs a, K line, K cluster, int warps, size_t smem, bool (*done)[kMaxDevices], cudaStream_t st) {
   set_groups(a, Q);
   const int units = a.groups * a.pool.n_kv_heads;
   const int ctas = paged_cluster(a.batch, units, a.cap, a.c, a.window, a.n_sink, KEYS, warps, kSms);
   if (ctas == 0) {
-    const bool by_warps = paged_solo(a.batch, units, kSms);
-    if (cudaError_t e = allow_smem(by_warps ? solo : line, smem, done[by_warps])) return e;
+    if (cudaError_t e = allow_smem(line, smem, done[0])) return e;
     return by_lines(a, KEYS, [&](const PagedAttnArgs &part) {
-      (by_warps ? solo : line)<<<kSms, warps * 32, smem, st>>>(part);
+      line<<<kSms, warps * 32, smem, st>>>(part);
       if (cudaError_t e = cudaGetLastError()) return e;
-      return launch_combine<HD, Q, KEYS>(part, by_warps ? kSms * warps : kSms, st);
+      return launch_combine<HD, Q, KEYS>(part, kSms * warps, st);
     });
   }
-  if (cudaError_t e = allow_smem(cluster, smem, done[2])) return e;
+  if (cudaError_t e = allow_smem(cluster, smem, done[1])) return e;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = dim3(ctas, units, a.batch); cfg.blockDim = dim3(warps * 32); cfg.dynamicSmemBytes = smem; cfg.stream = st;

@@ -120,7 +120,4 @@ inline bool paged_line_fits(int nq, int n_kv_heads, int hd, bool f32, int cap) {
   return line_batch(n_kv_heads * ((nq + q - 1) / q), cap, paged_keys(nq, hd, f32)) > 0;
 }
 
-// Whether every warp gets a piece of the line of its own.
-inline bool paged_solo(int batch, int units, int sms) { return (long long)batch * units >= 2 * sms; }
-
 }  // namespace fc

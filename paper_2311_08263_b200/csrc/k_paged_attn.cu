@@ -2,15 +2,17 @@
 //
 // paged_mma_kernel (bf16).  A unit is a kv head of a sequence and 8 or 16 queries (window rows x heads of the group); its keys come in tiles of
 // 16.  The products are taken with the keys as rows, S^T = K.Q^T and O^T = V^T.P^T, so that the 16 rows of an MMA are keys and
-// head elements, always full, and only its 8 columns are queries.  The warps of a CTA take turns at the tiles of its piece of work.  A warp loads its
-// own tiles into its own ring (cp.async, 16 bytes a lane; the lanes look up the pages of the tile's keys), so that it waits for nobody while it
-// streams.  Scores, probabilities and the output stay in its registers.  Where a unit (or the CTA's piece of it) ends, the warps
-// exchange their sums through shared memory and each adds up a part of the elements.
-//   Line: one CTA per SM.  The tiles of all units stand in one line, sequence by sequence, cut into equal pieces, one per CTA, whatever
-// the lengths: the launch depends on none, a batch of ragged caches is as balanced as one long cache, and the rings run on from unit to unit.  A
-// unit that several CTAs share goes to scratch as un-normalised sums, which paged_combine_kernel adds up in order.
-//   Cluster: for tables that hold little, a cluster per unit, whose CTAs take equal shares of its tiles and join them through distributed
-// shared memory: one launch, no scratch.
+// head elements, always full, and only its 8 columns are queries.  A warp loads its own tiles into its own ring (cp.async, 16 bytes a lane; the
+// lanes look up the pages of the tile's keys, a tile ahead), so that it waits for nobody while it streams.  Scores, probabilities and the output
+// stay in its registers.
+//   Line: one CTA per SM, eight warps.  The tiles of all units stand in one line, sequence by sequence, cut into equal pieces, one per warp,
+// whatever the lengths: the launch depends on none, a batch of ragged caches is as balanced as one long cache, and the rings run on from unit to
+// unit.  A unit that several warps share goes to scratch as un-normalised sums, which paged_combine_kernel adds up in order.
+//   (A piece per CTA, whose warps take turns at its tiles and exchange sums where a unit ends, leaves fewer parts but stalls at every end: 7B, 16 x 1 token over
+// 2048 keys 88 us against 79, 40 x 8 rows over 10 keys 52 against 12; only one sequence over 32000 keys was better, 87.6 against 91.)
+//   Cluster: for tables that hold little, a cluster per unit, whose warps take turns at the tiles.  They exchange their sums through shared memory, each
+// adds up a part of the elements, and the CTAs join theirs through distributed shared memory: one launch, no scratch.
+// Bound by HBM where there is much to read (7B, 16 x 1 token over 2048 keys: 6.0 TB/s), by latency below some 50 MB.
 //
 // Probabilities enter the tensor cores as three bf16 parts (their sum has all 24 bits), a tile's product is added to the output in fp32: what is rounded
 // is what is stored in the cache, nothing else.  (Two parts leave 1.5e-6, relative, of the result.)
@@ -40,14 +42,15 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
+
 // QN: blocks of 8 queries of a unit.  LINE: the line of tiles, else a cluster per unit (grid: CTAs of the cluster, units, sequences).
-template <int HD, int QN, Mode MODE>
+template <int HD, int QN, bool LINE>
 __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_constant__ PagedAttnArgs a) {
   using C = PagedCfg<HD>;
   constexpr int W = kWarps, S = C::S, KS = HD / 16, DB = C::DB, Q = 8 * QN;
   constexpr int PER = HD / 8;                            // 16-byte pieces of a row
   constexpr int OWN = (DB + W - 1) / W;                  // blocks of elements that a warp adds up
-  if (MODE != kCluster) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (LINE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
   __shared__ float2 ml[W][Q];                            // (max, sum) per warp and query
   __shared__ unsigned int bad_keys[W][S];                // keys of a tile whose page is missing
@@ -63,16 +66,15 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
   Place seg;                                             // where the segment (a unit's tiles in this CTA's piece) begins
   int n_mine;
-  // a warp that works on its own: consecutive pieces on different SMs
-  const int worker = MODE == kSolo ? warp * kSms + (int)blockIdx.x : (int)blockIdx.x;
-  if (!my_piece<kKeys, MODE>(a, worker, MODE == kSolo ? W * kSms : kSms, seg, n_mine)) return;
-  constexpr int STEP = MODE == kSolo ? 1 : W;
-  TileStream<kKeys, C::kRow, S, Q, MODE, W> stream(a, seg, MODE == kSolo ? 0 : warp, n_mine, ring, bad_keys[warp]);
+  const int worker = warp * kSms + (int)blockIdx.x;      // on the line: consecutive pieces on different SMs
+  if (!my_piece<kKeys, LINE>(a, worker, W * kSms, seg, n_mine)) return;
+  constexpr int STEP = LINE ? 1 : W;
+  TileStream<kKeys, C::kRow, S, Q, LINE, W> stream(a, seg, LINE ? 0 : warp, n_mine, ring, bad_keys[warp]);
 #pragma unroll 1
   for (int s = 0; s < S - 1; ++s) stream.request(s);
 
   int stage = 0;
-  int i = MODE == kSolo ? 0 : warp;                      // this warp's next tile in the piece
+  int i = LINE ? 0 : warp;                               // this warp's next tile in the piece
   int done = 0;                                          // tiles of the piece in front of the segment
   while (true) {
     // ---- a segment: tiles done .. done + seg_n of the piece, tiles seg.t .. of the unit
@@ -254,10 +256,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
         l_run[n][x] += __shfl_xor_sync(0xffffffffu, l_run[n][x], 4);
         l_run[n][x] += __shfl_xor_sync(0xffffffffu, l_run[n][x], 8);
         l_run[n][x] += __shfl_xor_sync(0xffffffffu, l_run[n][x], 16);
-        if (MODE != kSolo && g4 == 0) ml[warp][n * 8 + t4 * 2 + x] = make_float2(m_run[n][x], l_run[n][x]);
+        if (!LINE && g4 == 0) ml[warp][n * 8 + t4 * 2 + x] = make_float2(m_run[n][x], l_run[n][x]);
       }
-    const bool whole = MODE != kCluster ? seg_n == seg.k.n : gridDim.x == 1;
-    if (MODE == kSolo) {
+    const bool whole = LINE ? seg_n == seg.k.n : gridDim.x == 1;
+    if (LINE) {
       // ---- all of it is this warp's
       float *part = a.parts + ((long long)worker * 2 + (done > 0)) * part_floats(Q, HD);
 #pragma unroll
@@ -281,12 +283,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
       move_on<kKeys>(a, seg, seg_n);
       continue;
     }
-    // where sums go that are not the whole unit's: scratch, or this CTA's shared memory (the ring, drained)
-    float *part = MODE == kLine ? a.parts + ((long long)worker * 2 + (done > 0)) * part_floats(Q, HD) : reinterpret_cast<float *>(base_g);
-    if (MODE == kCluster) {
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      __syncthreads();
-    }
+    // sums that are not the whole unit's: this CTA's shared memory (the ring, drained)
+    float *part = reinterpret_cast<float *>(base_g);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
 #pragma unroll
     for (int n = 0; n < QN; ++n) {
       if (n) __syncthreads();
@@ -333,20 +333,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
           float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + (q - q0) * HD;
           to[d * 16 + g4] = sum[x] * f;
           to[d * 16 + g4 + 8] = sum[x + 2] * f;
-          if (!whole && d == 0 && g4 == 0) {
-            if (MODE == kLine) *reinterpret_cast<float2 *>(part + Q * HD + (q - q0) * 2) = make_float2(M[x], den[x]);
-            else ml_cta[q - q0] = make_float2(M[x], den[x]);
-          }
+          if (!whole && d == 0 && g4 == 0) ml_cta[q - q0] = make_float2(M[x], den[x]);
         }
       }
     }
-    if (MODE == kCluster) break;
-    done += seg_n;
-    if (done == n_mine) break;
-    move_on<kKeys>(a, seg, seg_n);
-    __syncthreads();                                     // the exchange buffers are free again
+    break;
   }
-  if (MODE != kCluster) {
+  if (LINE) {
     asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
@@ -358,8 +351,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
 // ------------------------------------------------------------------------------------ host side
 template <int HD, int QN>
 cudaError_t launch_mma(const PagedAttnArgs &a, cudaStream_t st) {
-  static bool done[3][kMaxDevices] = {};
-  return launch_units<HD, 8 * QN, kKeys>(a, paged_mma_kernel<HD, QN, kLine>, paged_mma_kernel<HD, QN, kSolo>, paged_mma_kernel<HD, QN, kCluster>, kWarps,
+  static bool done[2][kMaxDevices] = {};
+  return launch_units<HD, 8 * QN, kKeys>(a, paged_mma_kernel<HD, QN, true>, paged_mma_kernel<HD, QN, false>, kWarps,
                                          PagedCfg<HD>::kSmem, done, st);
 }
 template <int HD>

@@ -23,11 +23,11 @@ struct FmaCfg {
   static constexpr size_t kSmem = 128 + kRing + kP + (kQ + kExchange > kWarps * kQ ? kQ + kExchange : kWarps * kQ);
 };
 
-template <int HD, int QB, Mode MODE>
+template <int HD, int QB, bool LINE>
 __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_constant__ PagedAttnArgs a) {
   using C = FmaCfg<HD, QB>;
   constexpr int W = kWarps, S = C::S, KEYS = C::KEYS, E = HD / 32;
-  if (MODE != kCluster) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (LINE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
   __shared__ float2 ml[W][QB], ml_cta[QB];               // (max, sum)
   __shared__ unsigned int bad_keys[W][S];
@@ -38,34 +38,33 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
   const uint32_t ring = base + (uint32_t)warp * (S * C::kTile);
   float *ps = reinterpret_cast<float *>(base_g + C::kRing) + warp * KEYS * QB;
   // the unit's queries, and room for the exchange; a warp on its own has its queries where the others would exchange
-  float *qs = reinterpret_cast<float *>(base_g + C::kRing + C::kP) + (MODE == kSolo ? warp * QB * HD : 0);
+  float *qs = reinterpret_cast<float *>(base_g + C::kRing + C::kP) + (LINE ? warp * QB * HD : 0);
   float *exchange = reinterpret_cast<float *>(base_g + C::kRing + C::kP + C::kQ);
 
   const int group = a.group, nq = a.nq;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
   Place seg;
   int n_mine;
-  // a warp that works on its own: consecutive pieces on different SMs
-  const int worker = MODE == kSolo ? warp * kSms + (int)blockIdx.x : (int)blockIdx.x;
-  if (!my_piece<KEYS, MODE>(a, worker, MODE == kSolo ? W * kSms : kSms, seg, n_mine)) return;
-  constexpr int STEP = MODE == kSolo ? 1 : W;
-  TileStream<KEYS, C::kRow, S, QB, MODE, W> stream(a, seg, MODE == kSolo ? 0 : warp, n_mine, ring, bad_keys[warp]);
+  const int worker = warp * kSms + (int)blockIdx.x;      // on the line: consecutive pieces on different SMs
+  if (!my_piece<KEYS, LINE>(a, worker, W * kSms, seg, n_mine)) return;
+  constexpr int STEP = LINE ? 1 : W;
+  TileStream<KEYS, C::kRow, S, QB, LINE, W> stream(a, seg, LINE ? 0 : warp, n_mine, ring, bad_keys[warp]);
 #pragma unroll 1
   for (int s = 0; s < S - 1; ++s) stream.request(s);
 
   const int key = lane % KEYS, share = lane / KEYS;      // a lane's key, and which 32 elements of it
-  int stage = 0, i = MODE == kSolo ? 0 : warp, done = 0;
+  int stage = 0, i = LINE ? 0 : warp, done = 0;
   while (true) {
     // ---- a segment: tiles done .. done + seg_n of the piece, tiles seg.t .. of the unit
     const int seg_n = min(n_mine - done, seg.k.n - seg.t);
     const int q0 = seg.qg * QB, q_last = min(nq - 1, q0 + QB - 1);
-    // kSolo: the warps have places of their own for the queries
-    if (MODE == kSolo) __syncwarp();
-    for (int e = MODE == kSolo ? lane : tid; e < QB * (HD / 4); e += MODE == kSolo ? 32 : kThreads) {
+    // on the line the warps have places of their own for the queries
+    if (LINE) __syncwarp();
+    for (int e = LINE ? lane : tid; e < QB * (HD / 4); e += LINE ? 32 : kThreads) {
       const int n = e / (HD / 4), c4 = e - n * (HD / 4), q = min(q0 + n, nq - 1), j = quotient16(q, a.group_inv), h = seg.kvh * group + q - j * group;
       reinterpret_cast<float4 *>(qs)[e] = *reinterpret_cast<const float4 *>((const float *)a.q + ((long long)seg.b * a.c + j) * a.q_stride + h * HD + c4 * 4);
     }
-    if (MODE == kSolo) __syncwarp();
+    if (LINE) __syncwarp();
     else __syncthreads();
     int pos[QB];
     float m[QB], l[QB], o[QB][E];
@@ -183,11 +182,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
     for (int n = 0; n < QB; ++n) {
 #pragma unroll
       for (int d = 1; d < KEYS; d <<= 1) l[n] += __shfl_xor_sync(0xffffffffu, l[n], d);
-      if (MODE != kSolo && lane == 0) ml[warp][n] = make_float2(m[n], l[n]);
+      if (!LINE && lane == 0) ml[warp][n] = make_float2(m[n], l[n]);
     }
-    if (MODE == kCluster) asm volatile("cp.async.wait_all;" ::: "memory");
-    const bool whole = MODE != kCluster ? seg_n == seg.k.n : gridDim.x == 1;
-    if (MODE == kSolo) {
+    if (!LINE) asm volatile("cp.async.wait_all;" ::: "memory");
+    const bool whole = LINE ? seg_n == seg.k.n : gridDim.x == 1;
+    if (LINE) {
       // ---- all of it is this warp's
       float *part = a.parts + ((long long)worker * 2 + (done > 0)) * part_floats(QB, HD);
 #pragma unroll
@@ -206,8 +205,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
       move_on<KEYS>(a, seg, seg_n);
       continue;
     }
-    // sums that are not the whole unit's: scratch, or this CTA's shared memory (the ring, drained)
-    float *part = MODE == kLine ? a.parts + ((long long)worker * 2 + (done > 0)) * part_floats(QB, HD) : reinterpret_cast<float *>(base_g);
+    // sums that are not the whole unit's: this CTA's shared memory (the ring, drained)
+    float *part = reinterpret_cast<float *>(base_g);
 #pragma unroll
     for (int n0 = 0; n0 < QB; n0 += C::XQ) {
       if (n0) __syncthreads();
@@ -233,19 +232,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
         const float f = !whole ? 1.f : seg.len < 0 ? 0.f : result_scale(a, seg.len + j, den);
         float *to = whole ? a.out + (((long long)seg.b * a.c + j) * a.hq + h) * HD : part + n * HD;
         *reinterpret_cast<float4 *>(to + c4 * 4) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-        if (!whole && c4 == 0) {
-          if (MODE == kLine) *reinterpret_cast<float2 *>(part + QB * HD + n * 2) = make_float2(M, den);
-          else ml_cta[n] = make_float2(M, den);
-        }
+        if (!whole && c4 == 0) ml_cta[n] = make_float2(M, den);
       }
     }
-    if (MODE == kCluster) break;
-    done += seg_n;
-    if (done == n_mine) break;
-    move_on<KEYS>(a, seg, seg_n);
-    __syncthreads();                                     // the queries and the exchange are free again
+    break;
   }
-  if (MODE != kCluster) {
+  if (LINE) {
     asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
@@ -257,8 +249,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
 template <int HD, int QB>
 cudaError_t launch(const PagedAttnArgs &a, cudaStream_t st) {
   using C = FmaCfg<HD, QB>;
-  static bool done[3][kMaxDevices] = {};
-  return launch_units<HD, QB, C::KEYS>(a, paged_fma_kernel<HD, QB, kLine>, paged_fma_kernel<HD, QB, kSolo>, paged_fma_kernel<HD, QB, kCluster>, kWarps, C::kSmem,
+  static bool done[2][kMaxDevices] = {};
+  return launch_units<HD, QB, C::KEYS>(a, paged_fma_kernel<HD, QB, true>, paged_fma_kernel<HD, QB, false>, kWarps, C::kSmem,
                                        done, st);
 }
 template <int HD>

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
 
   Place seg;
   int n_mine;
-  if (!my_piece<kKeys, kLine>(a, blockIdx.x, kSms, seg, n_mine)) return;
+  if (!my_piece<kKeys, true>(a, blockIdx.x, kSms, seg, n_mine)) return;
 
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
