@@ -317,9 +317,10 @@ int fc_op_paged_store(const fc_pages *pages, int32_t layer, const int32_t *table
  * pool, or lies beyond the table, is NaN; pages that no row sees may be missing.  Keys and values that a row does not see do not reach
  * it, whatever they hold.  Results do not depend on the order in which the work runs.
  * c <= 64, n_heads <= 512 (else, and for tables of some ten million positions and many heads, FC_ERR_CAPACITY); q, out 16-byte aligned, q_stride a
- * multiple of 16 bytes; scratch: device, 256-byte aligned, at least
- * ..._scratch_bytes(...) bytes (0: shape refused), whatever the lengths; what it holds before and after means nothing. */
-size_t fc_op_paged_attention_scratch_bytes(int32_t batch, int32_t c, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype);
+ * multiple of 16 bytes; scratch: device, 256-byte aligned, at least ..._scratch_bytes(...) bytes for these arguments, whatever the lengths; what it holds
+ * before and after means nothing.  That function returns 0 for what is refused, and 256 where the call uses no scratch (which may be NULL then). */
+size_t fc_op_paged_attention_scratch_bytes(int32_t batch, int32_t c, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                           int32_t table_width, int32_t page_size, int32_t window, int32_t n_sink);
 int fc_op_paged_attention(const fc_pages *pages, int32_t layer, const int32_t *table, int32_t table_width, const int32_t *kv_len,
                           const void *q, int64_t q_stride, float *out, int32_t batch, int32_t c, int32_t n_heads, int32_t window,
                           int32_t n_sink, void *scratch, size_t scratch_bytes, void *cuda_stream);

@@ -373,11 +373,9 @@ cudaError_t launch_gemm_chain(const UmmaPlan *const *plans, const GemmArgs *args
 int pages_ok(const fc_pages *p);
 // Attention over pages (k_paged_attn.cu).
 struct PagedAttnArgs;
-size_t paged_attn_scratch(int nq, int hd, int dtype);       // nq: queries of a kv head
-size_t paged_umma_scratch(int hd);
+struct PagedPlan;
+cudaError_t launch_paged_attn(PagedAttnArgs a, const PagedPlan &plan, int dtype, int hd, cudaStream_t st);
+cudaError_t launch_paged_fma(const PagedAttnArgs &a, const PagedPlan &plan, int hd, cudaStream_t st);
 cudaError_t launch_paged_umma(PagedAttnArgs a, int hd, cudaStream_t st);
-size_t paged_fma_scratch(int hd);
-cudaError_t launch_paged_fma(const PagedAttnArgs &a, int hd, cudaStream_t st);
-cudaError_t launch_paged_attn(PagedAttnArgs a, int dtype, int hd, cudaStream_t st);
 
 }  // namespace fc

@@ -11,7 +11,7 @@ namespace fc {
 
 namespace {
 
-constexpr int kSms = 148;              // CTAs on the line: one per SM
+constexpr int kSms = kPagedSms;        // CTAs on the line: one per SM
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -399,27 +399,26 @@ cudaError_t by_lines(const PagedAttnArgs &all, int keys, F launch) {
   return cudaSuccess;
 }
 
-// The line, a piece for every warp, and the kernel that joins its parts; or clusters where paged_cluster says so.
+// The line, a piece for every warp, and the kernel that joins its parts; or clusters where the plan says so.
 template <int HD, int Q, int KEYS, typename K>
-cudaError_t launch_units(PagedAttnArgs a, K line, K cluster, int warps, size_t smem, bool (*done)[kMaxDevices], cudaStream_t st) {
+cudaError_t launch_units(PagedAttnArgs a, const PagedPlan &plan, K line, K cluster, size_t smem, bool (*done)[kMaxDevices], cudaStream_t st) {
+  if (plan.queries != Q || plan.keys != KEYS) return cudaErrorInvalidValue;
   set_groups(a, Q);
-  const int units = a.groups * a.pool.n_kv_heads;
-  const int ctas = paged_cluster(a.batch, units, a.cap, a.c, a.window, a.n_sink, KEYS, warps, kSms);
-  if (ctas == 0) {
+  if (plan.ctas == 0) {
     if (cudaError_t e = allow_smem(line, smem, done[0])) return e;
     return by_lines(a, KEYS, [&](const PagedAttnArgs &part) {
-      line<<<kSms, warps * 32, smem, st>>>(part);
+      line<<<kSms, kPagedWarps * 32, smem, st>>>(part);
       if (cudaError_t e = cudaGetLastError()) return e;
-      return launch_combine<HD, Q, KEYS>(part, kSms * warps, st);
+      return launch_combine<HD, Q, KEYS>(part, plan.workers, st);
     });
   }
   if (cudaError_t e = allow_smem(cluster, smem, done[1])) return e;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
-  cfg.gridDim = dim3(ctas, units, a.batch); cfg.blockDim = dim3(warps * 32); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.gridDim = dim3(plan.ctas, plan.units, a.batch); cfg.blockDim = dim3(kPagedWarps * 32); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[0].val.clusterDim.x = (unsigned)plan.ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, cluster, a);
 }

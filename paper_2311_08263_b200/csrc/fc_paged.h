@@ -1,5 +1,6 @@
 // Paged K/V cache: arguments of the kernels, and the index arithmetic they share with the host (compiles without CUDA).
 #pragma once
+#include <stddef.h>
 #include <stdint.h>
 
 #if defined(__CUDACC__)
@@ -99,25 +100,55 @@ inline int line_batch(int units, int cap, int keys) {
   return most > 0x7fffffff ? 0 : (int)(0x7fffffffll / most);
 }
 
+// ---- which kernel a call takes, and in which form
+// kFma: fp32 (k_paged_fma.cu); kMma: bf16 (k_paged_attn.cu); kUmma: bf16 on tcgen05 (k_paged_umma.cu).
+enum PagedKind { kFma, kMma, kUmma };
+struct PagedPlan {
+  PagedKind kind;
+  int queries, keys;      // of a unit, of a tile
+  int units;              // of a sequence
+  int ctas;               // CTAs of a cluster per unit; 0: the line
+  int workers;            // of the line
+  size_t scratch;         // bytes; 0 with clusters
+  bool fits;              // one sequence's tiles can be counted
+};
+constexpr int kPagedSms = 148, kPagedWarps = 8, kUmmaQueries = 128, kUmmaKeys = 64, kMmaKeys = 16;
+constexpr size_t kUmmaStatus = (kPagedSms * sizeof(unsigned int) + 255) / 256 * 256;
+
 // CTAs of a cluster per unit where one launch of clusters does the work of the line and the kernel that joins its parts, 0 otherwise.  All
 // clusters have to run at once, and no warp may have more than a few tiles, whatever the lengths are (only the table's bound on them is known).
-inline int paged_cluster(int batch, int units, int cap, int c, int window, int n_sink, int keys, int warps, int sms) {
-  const long long most = window > 0 && (long long)window + c + n_sink < cap ? (long long)window + c + n_sink + 2 * keys : cap;
-  const long long tiles = (most + keys - 1) / keys;
+inline int paged_cluster(int batch, int units, long long most_keys, int keys) {
+  const long long tiles = (most_keys + keys - 1) / keys;
   int ctas = 1;
-  while (ctas < 8 && tiles > ctas * warps && (long long)batch * units * ctas * 2 <= sms - 20) ctas *= 2;
-  return (long long)batch * units * ctas <= sms && tiles <= 4ll * warps * ctas ? ctas : 0;
+  while (ctas < 8 && tiles > ctas * kPagedWarps && (long long)batch * units * ctas * 2 <= kPagedSms - 20) ctas *= 2;
+  return (long long)batch * units * ctas <= kPagedSms && tiles <= 4ll * kPagedWarps * ctas ? ctas : 0;
 }
 
-// Whether the kernel on tcgen05 takes a kv head's nq queries.
-inline bool paged_umma(int nq, int hd) { return nq > 32 && hd >= 64; }
-// Queries of a unit and keys of a tile in fp32 (k_paged_fma.cu) and in bf16 (k_paged_attn.cu, k_paged_umma.cu).
-inline int paged_queries(int nq, int hd, bool f32) { return f32 ? (nq == 1 ? 1 : 8) : paged_umma(nq, hd) ? 128 : nq <= 8 ? 8 : 16; }
-inline int paged_keys(int nq, int hd, bool f32) { return f32 ? 1024 / hd : paged_umma(nq, hd) ? 64 : 16; }
-// Whether one sequence's tiles can be counted.
-inline bool paged_line_fits(int nq, int n_kv_heads, int hd, bool f32, int cap) {
-  const int q = paged_queries(nq, hd, f32);
-  return line_batch(n_kv_heads * ((nq + q - 1) / q), cap, paged_keys(nq, hd, f32)) > 0;
+// Whether tcgen05 pays: its units are 128 queries, used or not, and it starts and ends slowly.  By what both cost (microseconds, keys up to the
+// table's bound): 5 and 0.168 (hd 64) or 0.232 (hd 128) per 16 queries x 16 keys and SM, against 12 and 1.09 or 2.3 per unit's tile of 64 keys and SM.
+// Measured, mma.sync against tcgen05: hd 128, 4 x 32 heads x 64 rows over 1000 keys 59.4, 45.6 us; 8 x 8 heads x 64 queries over 2000 63.1, 44.2; 1 x 8 x 64
+// over 4000 26.7, 29.9; 1 x 8 x 128 over 1000 13.3, 21.3; 8 x 40 x 32 over 1024 72, 90; hd 64, 16 x 4 x 128 over 641 28.9, 20.5, 4 x 4 x 128 17.1, 16.4, 1 x 4 x 128 7.7, 12.7.
+inline bool umma_pays(int batch, int n_kv_heads, int nq, int hd, long long most_keys) {
+  if (nq <= 32 || hd < 64) return false;
+  const double heads = (double)batch * n_kv_heads / kPagedSms;
+  const double mma = 5 + heads * ((nq + 15) / 16) * (most_keys / 16.0) * (hd == 128 ? 0.232 : 0.168);
+  const double umma = 12 + heads * ((nq + 127) / 128) * (most_keys / 64.0) * (hd == 128 ? 2.3 : 1.09);
+  return umma < mma;
+}
+
+inline PagedPlan paged_plan(int batch, int c, int hq, int hkv, int hd, bool f32, int cap, int window, int n_sink) {
+  PagedPlan p;
+  const int nq = hq / hkv * c;
+  const long long bound = (long long)window + c + n_sink + 2 * kMmaKeys, most = window > 0 && bound < cap ? bound : cap;      // keys of a sequence
+  p.kind = f32 ? kFma : umma_pays(batch, hkv, nq, hd, most) ? kUmma : kMma;
+  p.queries = p.kind == kUmma ? kUmmaQueries : p.kind == kFma && nq == 1 ? 1 : p.kind == kFma || nq <= 8 ? 8 : 16;
+  p.keys = p.kind == kUmma ? kUmmaKeys : p.kind == kFma ? 1024 / hd : kMmaKeys;
+  p.units = hkv * ((nq + p.queries - 1) / p.queries);
+  p.ctas = p.kind == kUmma ? 0 : paged_cluster(batch, p.units, most, p.keys);
+  p.workers = p.kind == kUmma ? kPagedSms : kPagedSms * kPagedWarps;
+  p.scratch = p.ctas ? 0 : (p.kind == kUmma ? kUmmaStatus : 0) + (size_t)p.workers * 2 * part_floats(p.queries, hd) * sizeof(float);
+  p.fits = line_batch(p.units, cap, p.keys) > 0;
+  return p;
 }
 
 }  // namespace fc

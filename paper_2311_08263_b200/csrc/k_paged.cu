@@ -131,11 +131,16 @@ extern "C" int fc_op_paged_store(const fc_pages *pages, int32_t layer, const int
   return cudaGetLastError() == cudaSuccess ? FC_OK : FC_ERR_CUDA;
 }
 
+// The smallest size that is given out: such a call uses no scratch.
+constexpr size_t kNoScratch = 256;
+
 extern "C" size_t fc_op_paged_attention_scratch_bytes(int32_t batch, int32_t c, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
-                                                      int32_t dtype) {
-  if (batch < 1 || c < 1 || c > 64 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return 0;
+                                                      int32_t dtype, int32_t table_width, int32_t page_size, int32_t window, int32_t n_sink) {
+  if (batch < 1 || c < 1 || c > 64 || n_heads < 1 || n_heads > 512 || n_kv_heads < 1 || n_heads % n_kv_heads) return 0;
   if ((head_dim != 32 && head_dim != 64 && head_dim != 128) || (dtype != FC_F32 && dtype != FC_BF16)) return 0;
-  return (paged_attn_scratch(n_heads / n_kv_heads * c, head_dim, dtype) + 255) / 256 * 256;
+  if (table_width < 1 || page_size < 1 || (long long)table_width * page_size > INT_MAX - 1024 || window < 0 || n_sink < 0) return 0;
+  const PagedPlan plan = paged_plan(batch, c, n_heads, n_kv_heads, head_dim, dtype == FC_F32, table_width * page_size, window, window > 0 ? n_sink : 0);
+  return !plan.fits ? 0 : plan.scratch == 0 ? kNoScratch : kNoScratch + (plan.scratch + 255) / 256 * 256;
 }
 
 extern "C" int fc_op_paged_attention(const fc_pages *pages, int32_t layer, const int32_t *table, int32_t table_width, const int32_t *kv_len,
@@ -143,13 +148,15 @@ extern "C" int fc_op_paged_attention(const fc_pages *pages, int32_t layer, const
                                      int32_t window, int32_t n_sink, void *scratch, size_t scratch_bytes, void *cuda_stream) {
   if (int rc = call_ok(pages, layer, table, table_width, kv_len, batch, c, n_heads)) return rc;
   const int hd = pages->head_dim, per = pages->dtype == FC_F32 ? 4 : 8;
-  if (!q || !out || !scratch || ((uintptr_t)q | (uintptr_t)out) % 16 || (uintptr_t)scratch % 256 || q_stride % per ||
+  if (!q || !out || ((uintptr_t)q | (uintptr_t)out) % 16 || (uintptr_t)scratch % 256 || q_stride % per ||
       q_stride < (int64_t)n_heads * hd || window < 0 || n_sink < 0) return FC_ERR_ARG;
-  if (scratch_bytes < fc_op_paged_attention_scratch_bytes(batch, c, n_heads, pages->n_kv_heads, hd, pages->dtype)) return FC_ERR_CAPACITY;
-  if (!paged_line_fits(n_heads / pages->n_kv_heads * c, pages->n_kv_heads, hd, pages->dtype == FC_F32, table_width * pages->page_size)) return FC_ERR_CAPACITY;
   PagedAttnArgs a; memset(&a, 0, sizeof a);
   a.pool = view_of(pages, layer);
   a.table = table; a.width = table_width; a.cap = table_width * pages->page_size; a.kv_len = kv_len; a.q = q; a.q_stride = q_stride; a.out = out;
   a.batch = batch; a.c = c; a.hq = n_heads; a.window = window; a.n_sink = window > 0 ? n_sink : 0; a.parts = (float *)scratch;
-  return launch_paged_attn(a, pages->dtype, hd, (cudaStream_t)cuda_stream) == cudaSuccess ? FC_OK : FC_ERR_CUDA;
+  const PagedPlan plan = paged_plan(batch, c, n_heads, pages->n_kv_heads, hd, pages->dtype == FC_F32, a.cap, window, a.n_sink);
+  if (!plan.fits) return FC_ERR_CAPACITY;
+  if (plan.scratch && !scratch) return FC_ERR_ARG;
+  if (scratch_bytes < plan.scratch) return FC_ERR_CAPACITY;
+  return launch_paged_attn(a, plan, pages->dtype, hd, (cudaStream_t)cuda_stream) == cudaSuccess ? FC_OK : FC_ERR_CUDA;
 }

@@ -22,8 +22,8 @@ namespace fc {
 
 namespace {
 
-constexpr int kKeys = 16;              // keys per tile
-constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kKeys = kMmaKeys;        // per tile
+constexpr int kWarps = kPagedWarps, kThreads = kWarps * 32;
 
 template <int HD>
 struct PagedCfg {
@@ -350,31 +350,24 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
 
 // ------------------------------------------------------------------------------------ host side
 template <int HD, int QN>
-cudaError_t launch_mma(const PagedAttnArgs &a, cudaStream_t st) {
+cudaError_t launch_mma(const PagedAttnArgs &a, const PagedPlan &plan, cudaStream_t st) {
   static bool done[2][kMaxDevices] = {};
-  return launch_units<HD, 8 * QN, kKeys>(a, paged_mma_kernel<HD, QN, true>, paged_mma_kernel<HD, QN, false>, kWarps,
-                                         PagedCfg<HD>::kSmem, done, st);
+  return launch_units<HD, 8 * QN, kKeys>(a, plan, paged_mma_kernel<HD, QN, true>, paged_mma_kernel<HD, QN, false>, PagedCfg<HD>::kSmem, done, st);
 }
 template <int HD>
-cudaError_t launch_hd(const PagedAttnArgs &a, cudaStream_t st) {
-  const int nq = a.hq / a.pool.n_kv_heads * a.c;
-  if (paged_umma(nq, HD)) return launch_paged_umma(a, HD, st);
-  return nq <= 8 ? launch_mma<HD, 1>(a, st) : launch_mma<HD, 2>(a, st);
+cudaError_t launch_hd(const PagedAttnArgs &a, const PagedPlan &plan, cudaStream_t st) {
+  return plan.queries == 8 ? launch_mma<HD, 1>(a, plan, st) : launch_mma<HD, 2>(a, plan, st);
 }
 
 }  // namespace
 
-size_t paged_attn_scratch(int nq, int hd, int dtype) {
-  if (dtype == FC_F32) return paged_fma_scratch(hd);
-  return paged_umma(nq, hd) ? paged_umma_scratch(hd) : (size_t)kSms * kWarps * 2 * part_floats(16, hd) * sizeof(float);
-}
-
-cudaError_t launch_paged_attn(PagedAttnArgs a, int dtype, int hd, cudaStream_t st) {
+cudaError_t launch_paged_attn(PagedAttnArgs a, const PagedPlan &plan, int dtype, int hd, cudaStream_t st) {
   const int es = dtype == FC_F32 ? 4 : 2;
   a.hd = hd; a.elem_bytes = es;
   a.page_bytes = a.pool.page_stride * es; a.head_bytes = a.pool.head_stride * es; a.slot_bytes = a.pool.slot_stride * es;
-  if (dtype == FC_F32) return launch_paged_fma(a, hd, st);
-  return hd == 128 ? launch_hd<128>(a, st) : hd == 64 ? launch_hd<64>(a, st) : launch_hd<32>(a, st);
+  if (plan.kind == kFma) return launch_paged_fma(a, plan, hd, st);
+  if (plan.kind == kUmma) return launch_paged_umma(a, hd, st);
+  return hd == 128 ? launch_hd<128>(a, plan, st) : hd == 64 ? launch_hd<64>(a, plan, st) : launch_hd<32>(a, plan, st);
 }
 
 }  // namespace fc

@@ -9,7 +9,7 @@ namespace fc {
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kWarps = kPagedWarps, kThreads = kWarps * 32;
 
 template <int HD, int QB>
 struct FmaCfg {
@@ -247,23 +247,20 @@ __global__ void __launch_bounds__(kThreads, 1) paged_fma_kernel(const __grid_con
 }
 
 template <int HD, int QB>
-cudaError_t launch(const PagedAttnArgs &a, cudaStream_t st) {
+cudaError_t launch(const PagedAttnArgs &a, const PagedPlan &plan, cudaStream_t st) {
   using C = FmaCfg<HD, QB>;
   static bool done[2][kMaxDevices] = {};
-  return launch_units<HD, QB, C::KEYS>(a, paged_fma_kernel<HD, QB, true>, paged_fma_kernel<HD, QB, false>, kWarps, C::kSmem,
-                                       done, st);
+  return launch_units<HD, QB, C::KEYS>(a, plan, paged_fma_kernel<HD, QB, true>, paged_fma_kernel<HD, QB, false>, C::kSmem, done, st);
 }
 template <int HD>
-cudaError_t launch_hd(const PagedAttnArgs &a, cudaStream_t st) {
-  return a.hq / a.pool.n_kv_heads * a.c == 1 ? launch<HD, 1>(a, st) : launch<HD, 8>(a, st);
+cudaError_t launch_hd(const PagedAttnArgs &a, const PagedPlan &plan, cudaStream_t st) {
+  return plan.queries == 1 ? launch<HD, 1>(a, plan, st) : launch<HD, 8>(a, plan, st);
 }
 
 }  // namespace
 
-size_t paged_fma_scratch(int hd) { return (size_t)kSms * kWarps * 2 * part_floats(8, hd) * sizeof(float); }
-
-cudaError_t launch_paged_fma(const PagedAttnArgs &a, int hd, cudaStream_t st) {
-  return hd == 128 ? launch_hd<128>(a, st) : hd == 64 ? launch_hd<64>(a, st) : launch_hd<32>(a, st);
+cudaError_t launch_paged_fma(const PagedAttnArgs &a, const PagedPlan &plan, int hd, cudaStream_t st) {
+  return hd == 128 ? launch_hd<128>(a, plan, st) : hd == 64 ? launch_hd<64>(a, plan, st) : launch_hd<32>(a, plan, st);
 }
 
 }  // namespace fc

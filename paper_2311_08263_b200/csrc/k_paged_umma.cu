@@ -17,7 +17,7 @@ namespace fc {
 
 namespace {
 
-constexpr int kKeys = 64, kQueries = 128;
+constexpr int kKeys = kUmmaKeys, kQueries = kUmmaQueries;
 constexpr int kThreads = 384;
 constexpr int kSoftRegs = 224, kLoadRegs = 56;           // registers a thread: 256 x 224 + 128 x 56 = 384 x 168, what the launch holds
 constexpr int kCopyWarps = 2;                            // that load tiles where TMA does not
@@ -666,16 +666,12 @@ cudaError_t launch(const PageMaps &maps, const PagedAttnArgs &a, cudaStream_t st
   });
 }
 
-size_t status_bytes() { return (kSms * sizeof(unsigned int) + 255) / 256 * 256; }
-
 }  // namespace
-
-size_t paged_umma_scratch(int hd) { return status_bytes() + (size_t)kSms * 2 * part_floats(kQueries, hd) * sizeof(float); }
 
 cudaError_t launch_paged_umma(PagedAttnArgs a, int hd, cudaStream_t st) {
   set_groups(a, kQueries);
   a.status = (unsigned int *)a.parts;
-  a.parts = (float *)((char *)a.parts + status_bytes());
+  a.parts = (float *)((char *)a.parts + kUmmaStatus);
   PageMaps maps;
   memset(&maps, 0, sizeof maps);
   if (page_maps(a, hd, &maps)) return hd == 128 ? launch<128, true>(maps, a, st) : launch<64, true>(maps, a, st);

@@ -377,11 +377,11 @@ def fc_op_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tab
     row, elem = q.stride()
     if q.dtype is not k.dtype or q.shape != (B * c, n_heads * hd) or elem != 1 or q.get_device() != device:
         raise ValueError("q: [B * c, n_heads * head size] in the pool's type with adjacent elements, on the pool's device")
-    nbytes = _scratch_bytes("fc_op_paged_attention_scratch_bytes", B, c, n_heads, pool.n_kv_heads, hd, pool.dtype)
-    scratch = torch.empty(nbytes, dtype=torch.uint8, device=k.device)
+    nbytes = _scratch_bytes("fc_op_paged_attention_scratch_bytes", B, c, n_heads, pool.n_kv_heads, hd, pool.dtype, width, pool.page_size, window, n_sink)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=k.device) if nbytes > 256 else None         # 256: none is used
     out = torch.empty(B * c, n_heads * hd, dtype=torch.float32, device=k.device)
     _enqueue(device, _l.load().fc_op_paged_attention, pool, 0, tab, width, _lengths(kv_len, B, device), q.data_ptr(), row, out.data_ptr(), B, c,
-             n_heads, window, n_sink, scratch.data_ptr(), nbytes)
+             n_heads, window, n_sink, scratch.data_ptr() if scratch is not None else None, nbytes)
     return out
 
 

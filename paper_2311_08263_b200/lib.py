@@ -117,7 +117,7 @@ def load() -> C.CDLL:
     i64, pg = C.c_int64, C.POINTER(fc_pages)
     lib.fc_op_paged_store.argtypes = [pg, i32, vp, i32, vp, vp, i64, vp, i32, i32, i32, C.c_float, vp]
     lib.fc_op_paged_attention_scratch_bytes.restype = C.c_size_t
-    lib.fc_op_paged_attention_scratch_bytes.argtypes = [i32] * 6
+    lib.fc_op_paged_attention_scratch_bytes.argtypes = [i32] * 10
     lib.fc_op_paged_attention.argtypes = [pg, i32, vp, i32, vp, vp, i64, vp] + [i32] * 5 + [vp, C.c_size_t, vp]
     lib.fc_op_pages_fork.argtypes = [vp, i32, i32, vp, vp, i32, i32, vp, vp, i32, vp]
     lib.fc_op_pages_free.argtypes = [vp, i32, i32, vp, vp, i32, i32, vp, i32, i32, i32, vp]

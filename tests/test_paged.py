@@ -31,7 +31,7 @@ def _store(l, pool=None, layer=0, table=P, width=5, kv_len=P, qkv=P, stride=16 *
 
 
 def _attention(l, pool=None, layer=0, table=P, width=5, kv_len=P, q=P, stride=8 * 64, out=P, batch=3, c=2, hq=8, window=0, n_sink=0,
-               scratch=P, nbytes=1 << 40):
+               scratch=P, nbytes=1 << 40):                      # long enough for the line: scratch is used
     return l.fc_op_paged_attention(_pool() if pool is None else pool, layer, table, width, kv_len, q, stride, out, batch, c, hq, window, n_sink, scratch,
                                    nbytes, None)
 
@@ -93,18 +93,23 @@ def test_store_refusals(l, kw, code):
 @pytest.mark.parametrize("kw,code", [
     (dict(layer=-1), -1), (dict(layer=2), -1), (dict(table=None), -1), (dict(width=0), -1), (dict(kv_len=None), -1), (dict(q=None), -1), (dict(q=P + 8), -1),
     (dict(stride=8 * 64 - 8), -1), (dict(stride=8 * 64 + 4), -1), (dict(out=None), -1), (dict(out=P + 4), -1), (dict(batch=0), -1), (dict(c=0), -1),
-    (dict(c=65), -1), (dict(hq=6), -1), (dict(window=-1), -1), (dict(n_sink=-1), -1), (dict(scratch=None), -1), (dict(scratch=P + 16), -1),
-    (dict(nbytes=0), lib.FC_ERR_CAPACITY), (dict(width=1 << 28), lib.FC_ERR_CAPACITY)])
+    (dict(c=65), -1), (dict(hq=6), -1), (dict(window=-1), -1), (dict(n_sink=-1), -1), (dict(width=5000, scratch=None), -1), (dict(scratch=P + 16), -1),
+    (dict(width=5000, nbytes=1000), lib.FC_ERR_CAPACITY), (dict(width=1 << 28), lib.FC_ERR_CAPACITY),
+    (dict(width=2 ** 31 // 16 - 100, c=64, hq=512, stride=512 * 64), lib.FC_ERR_CAPACITY), (dict(hq=516, stride=516 * 64), lib.FC_ERR_CAPACITY)])
 def test_attention_refusals(l, kw, code):
     assert _attention(l, **kw) == code
 
 
 def test_attention_scratch_bytes(l):
     size = l.fc_op_paged_attention_scratch_bytes
-    good = size(3, 2, 8, 4, 64, lib.FC_BF16)
-    assert good > 0 and good % 256 == 0
-    for bad in ((0, 2, 8, 4, 64, 1), (3, 0, 8, 4, 64, 1), (3, 65, 8, 4, 64, 1), (3, 2, 7, 4, 64, 1), (3, 2, 8, 0, 64, 1), (3, 2, 8, 4, 80, 1), (3, 2, 8, 4, 64, 2)):
-        assert size(*bad) == 0
+    args = dict(batch=3, c=2, hq=8, hkv=4, hd=64, dtype=lib.FC_BF16, width=5000, page=16, window=0, n_sink=0)
+    good = size(*args.values())
+    assert good > 256 and good % 256 == 0
+    assert size(*dict(args, width=5).values()) == 256                      # clusters: none is used
+    assert size(*dict(args, window=64).values()) == 256
+    for bad in (dict(batch=0), dict(c=0), dict(c=65), dict(hq=7), dict(hq=516), dict(hkv=0), dict(hd=80), dict(dtype=2), dict(width=0), dict(page=0),
+                dict(width=1 << 28), dict(window=-1), dict(n_sink=-1)):
+        assert size(*dict(args, **bad).values()) == 0
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -224,10 +229,13 @@ void key_tiles(int len, int rows, int cap, int w, int s, int keys, int *out) {
 int chunk_of(int total, int n) { return fc::chunk_of(total, n); }
 int quotient16(int x, int n) { return fc::quotient16(x, fc::reciprocal16(n)); }
 int line_batch(int u, int cap, int k) { return fc::line_batch(u, cap, k); }
-int line_fits(int nq, int hkv, int hd, int f32, int cap) { return fc::paged_line_fits(nq, hkv, hd, f32 != 0, cap); }
+void plan(int b, int c, int hq, int hkv, int hd, int f32, int cap, int w, int s, long long *out) {
+  const fc::PagedPlan p = fc::paged_plan(b, c, hq, hkv, hd, f32 != 0, cap, w, s);
+  out[0] = p.kind; out[1] = p.queries; out[2] = p.keys; out[3] = p.units; out[4] = p.ctas; out[5] = p.workers; out[6] = (long long)p.scratch; out[7] = p.fits;
+}
 void unit_parts(int begin, int n, int chunk, int *out) { const fc::UnitParts p = fc::unit_parts(begin, n, chunk); out[0] = p.first; out[1] = p.last; }
 int part_place(int begin, int worker, int chunk) { return fc::part_place(begin, worker, chunk); }
-int paged_cluster(int b, int u, int cap, int c, int w, int s, int keys, int warps, int sms) { return fc::paged_cluster(b, u, cap, c, w, s, keys, warps, sms); }
+
 }
 """)
     subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", build.CSRC, "-I", build.INCLUDE, str(src), "-o", str(so)])
@@ -308,8 +316,6 @@ def test_numbers_of_the_line_stay_within_31_bits(parts):
         n = parts.line_batch(units, cap, keys)
         most = units * -(-cap // keys)
         assert n * most < 2 ** 31 and (n == 0) == (units * (cap // keys + 1) >= 2 ** 31)
-    assert parts.line_fits(16, 32, 128, 0, 2 ** 24) and not parts.line_fits(16, 512, 128, 0, 2 ** 31 - 1024)
-    assert parts.line_fits(1, 32, 128, 1, 2 ** 24) and not parts.line_fits(64, 64, 128, 1, 2 ** 30)
 
 
 def test_queries_are_divided_exactly(parts):
@@ -317,14 +323,35 @@ def test_queries_are_divided_exactly(parts):
         assert all(parts.quotient16(x, n) == x // n for x in range(0, 65536, 7 if n > 16 else 1))
 
 
-def test_clusters_only_where_they_all_run_at_once_and_have_little_to_do(parts):
+def _plan(parts, *args):
+    out = (C.c_longlong * 8)()
+    parts.plan(*args, out)
+    return dict(zip(("kind", "queries", "keys", "units", "ctas", "workers", "scratch", "fits"), out))
+
+
+def test_plans(parts):
+    """Kernels and forms: clusters only where they all run at once and no warp has more than four tiles; scratch for the parts of every worker."""
     for batch in (1, 2, 16, 200):
-        for units in (1, 4, 32, 40, 148, 149):
-            for cap in (16, 500, 832, 4096, 100000):
-                for window in (0, 64):
-                    n = parts.paged_cluster(batch, units, cap, 4, window, 4, 16, 8, 148)
-                    assert n in (0, 1, 2, 4, 8)
-                    if n:
-                        assert batch * units * n <= 148
-                        keys = cap if not window else min(cap, window + 4 + 4 + 32)
-                        assert keys <= n * 8 * 4 * 16
+        for hkv in (1, 4, 32, 40):
+            for group in (1, 8):
+                for c in (1, 5, 16, 64):
+                    for hd in (32, 64, 128):
+                        for f32 in (0, 1):
+                            for cap in (16, 500, 832, 4096, 100000):
+                                for window in (0, 64):
+                                    p = _plan(parts, batch, c, hkv * group, hkv, hd, f32, cap, window, 4)
+                                    nq = group * c
+                                    assert p["fits"] and p["units"] == hkv * -(-nq // p["queries"])
+                                    assert (p["kind"] == 0) == bool(f32) and (p["kind"] != 2 or (nq > 32 and hd >= 64))
+                                    assert p["queries"] in ({0: (1, 8), 1: (8, 16), 2: (128,)}[p["kind"]])
+                                    if p["ctas"]:
+                                        assert p["kind"] != 2 and batch * p["units"] * p["ctas"] <= 148 and p["scratch"] == 0
+                                        assert (min(cap, window + c + 4 + 32) if window else cap) <= p["ctas"] * 8 * 4 * p["keys"]
+                                    else:
+                                        assert p["scratch"] >= p["workers"] * 2 * 4 * p["queries"] * (hd + 2)
+    assert not _plan(parts, 1, 64, 512, 64, 128, 1, 2 ** 30, 0, 0)["fits"]
+    # where each of the two bf16 kernels was measured to be the faster one
+    for args, kind in (((4, 64, 32, 32, 128, 0, 1064, 0, 0), 2), ((8, 16, 32, 8, 128, 0, 2016, 0, 0), 2), ((16, 16, 32, 4, 64, 0, 4112, 0, 0), 2),
+                       ((1, 16, 32, 8, 128, 0, 4016, 0, 0), 1), ((8, 32, 40, 40, 128, 0, 1056, 0, 0), 1), ((1, 16, 32, 4, 64, 0, 657, 0, 0), 1),
+                       ((4, 51, 32, 32, 128, 0, 64, 0, 0), 1)):
+        assert _plan(parts, *args)["kind"] == kind
