@@ -392,6 +392,7 @@ cudaError_t by_lines(const PagedAttnArgs &all, int keys, F launch) {
     a.batch = all.batch - b0 < most ? all.batch - b0 : most;
     a.table += (long long)b0 * a.width;
     a.kv_len += b0;
+    a.first = b0;
     a.q = (const char *)a.q + (long long)b0 * a.c * a.q_stride * a.elem_bytes;
     a.out += (long long)b0 * a.c * a.hq * all.hd;
     if (cudaError_t e = launch(a)) return e;

@@ -29,7 +29,7 @@ struct PagedAttnArgs {
   // set by the launcher: the queries' arithmetic (reciprocal of the heads of a group), the pool's strides in bytes
   int group, nq, groups;  // heads of a group, queries of a kv head, units of a kv head
   unsigned int group_inv;
-  int hd, elem_bytes;
+  int hd, elem_bytes, first;      // first: the sequence of the call that this launch begins with
   long long page_bytes, head_bytes, slot_bytes;
   float *parts;           // scratch: two parts per worker, [queries][hd] sums and [queries] (max, sum)
   unsigned int *status;   // scratch of the kernel that has waits, else null: per worker, 1 where a wait ran out

@@ -8,8 +8,11 @@
 //     fp32 (the tensor core's own additions are not rounded to nearest), a tile later, when it has long been there.  While one group does
 //     this the tensor core works for the other.  Where a segment ends, the groups join through shared memory.
 //   the third: a warp issues the first product, one the second; two load tiles, keys and values by TMA, a box per page and sub-tile (pages of
-//     whole groups of eight slots), or in turn by cp.async (any other page), and the queries of a unit in front of its first tile.
+//     whole groups of eight slots), or in turn by cp.async (any other page), and the queries of a unit in front of its first tile (by TMA with the
+//     keys where the heads of a group divide 128: the keys' warp runs tiles ahead, and a box of them is here sooner than 128 rows of copies).
 // Every wait is bounded: where one runs out the CTA says so in its status word, and the joining kernel writes NaN for what it was to compute.
+#include <type_traits>
+
 #include "fc_paged.cuh"
 #include "fc_plan.h"
 
@@ -113,9 +116,11 @@ __device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap *map, co
 }
 
 // Tensor maps of keys and values: dimension 0 are the elements; which of 1 .. 3 are slots, heads and pages.  box: slots that one load takes.
+// Of the queries: elements, heads of a group, rows, kv heads, a unit per box, where the heads of a group divide 128 (q_rows: window rows of a box;
+// 0: the queries are copied by a warp).
 struct PageMaps {
-  CUtensorMap k, v;
-  int slot_dim, head_dim, page_dim, box;
+  CUtensorMap k, v, q;
+  int slot_dim, head_dim, page_dim, box, q_rows;
 };
 
 template <int HD, bool TMA>
@@ -125,7 +130,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) unsigned long long k_full[S], v_full[S], k_empty[S], v_empty[S], q_full[2], q_free[2], s_ready[2], s_free[2], p_ready[2], o_ready[2], ex_full, ex_free,
-      drained[2], odd_bar[2];
+      drained[2], odd_bar[2], tmem_here;
   __shared__ unsigned int tmem_base_s, bad_keys[S][2], odd_keys[2][2];
   __shared__ int gave_up;
   __shared__ float2 ml[kQueries];
@@ -136,10 +141,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   const uint32_t q_base = base + S * C::kTile;
   float4 *exchange = reinterpret_cast<float4 *>(base_g + S * C::kTile + 2 * C::kQ);      // piece c4 of row r at r * 16 + (c4 ^ (r & 15))
 
-  Place seg;
-  int n_mine;
-  if (!my_piece<kKeys, true>(a, blockIdx.x, kSms, seg, n_mine)) return;
-
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
       mbar_init(smem_u32(&k_full[i]), 1); mbar_init(smem_u32(&v_full[i]), 1); mbar_init(smem_u32(&k_empty[i]), 1); mbar_init(smem_u32(&v_empty[i]), 1);
@@ -149,17 +150,29 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       mbar_init(smem_u32(&s_free[i]), 128); mbar_init(smem_u32(&p_ready[i]), 128); mbar_init(smem_u32(&odd_bar[i]), 128); mbar_init(smem_u32(&drained[i]), 1);
       odd_keys[i][0] = odd_keys[i][1] = 0u;
     }
-    mbar_init(smem_u32(&ex_full), 128); mbar_init(smem_u32(&ex_free), 128);
+    mbar_init(smem_u32(&ex_full), 128); mbar_init(smem_u32(&ex_free), 128); mbar_init(smem_u32(&tmem_here), 1);
     gave_up = 0;
     fence_barrier_init();
     fence_proxy_async();
   }
-  if (warp == 8) tmem_alloc(smem_u32(&tmem_base_s), 512);
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = tmem_base_s;                     // group w from column 256 w
+  Place seg;
+  int n_mine;
+  if (!my_piece<kKeys, true>(a, blockIdx.x, kSms, seg, n_mine)) return;
+  // tensor memory comes while the loads begin; whoever uses it waits for it
+  if (warp == 8) {
+    tmem_alloc(smem_u32(&tmem_base_s), 512);
+    tc_fence_before();
+    if (lane == 0) mbar_arrive(smem_u32(&tmem_here));
+  }
   volatile int *quit = &gave_up;
+  // Where tensor memory begins (group w from column 256 w), to a whole warp; false if it did not come.
+  auto tensor_memory = [&](uint32_t &t) {
+    if (!mbar_wait_warp(smem_u32(&tmem_here), 0, quit)) return false;
+    tc_fence_after();
+    t = __shfl_sync(0xffffffffu, *(volatile unsigned int *)&tmem_base_s, 0);
+    return true;
+  };
   const int group = a.group, nq = a.nq;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
 
@@ -198,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
     };
     // The two warps that issue MMAs run as one, on values that are broadcast from their first lane, and one thread is elected to issue:
     // descriptors are then worked out once in uniform registers.  (Inside `if (lane == 0)` an MMA cost the issuing thread about 60 cycles.)
-    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), tiles = __shfl_sync(0xffffffffu, base, 0);
+    const uint32_t tiles = __shfl_sync(0xffffffffu, base, 0);
     const int n_all = __shfl_sync(0xffffffffu, n_mine, 0);
     if (warp == 8) {
       // ------------------------------------------------------------------------------------------ S = Q.K^T
@@ -206,7 +219,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       int so = 0, left = min(n_all, seg.k.n - seg.t);    // ordinal of the segment, its tiles that are left
       Place at = seg;
       bool first = true;
-      for (int i = 0; i < n_all; ++i) {
+      uint32_t tm = 0;
+      const bool got = tensor_memory(tm);
+      for (int i = 0; got && i < n_all; ++i) {
         const int st = i % S, w = i & 1;
         if (first && !mbar_wait_warp(smem_u32(&q_full[so & 1]), (uint32_t)(so >> 1) & 1u, quit)) break;
         if (!mbar_wait_warp(smem_u32(&k_full[st]), (uint32_t)(i / S) & 1u, quit)) break;
@@ -235,7 +250,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
     } else if (warp == 11) {
       // ------------------------------------------------------------------------------------------ O = P.V
       constexpr uint32_t id_o = make_idesc(HD) | (1u << 16);       // V: N adjacent
-      for (int i = 0; i < n_all; ++i) {
+      uint32_t tm = 0;
+      const bool got = tensor_memory(tm);
+      for (int i = 0; got && i < n_all; ++i) {
         const int st = i % S, w = i & 1;
         if (!mbar_wait_warp(smem_u32(&v_full[st]), (uint32_t)(i / S) & 1u, quit)) break;
         if (!mbar_wait_warp(smem_u32(&p_ready[w]), (uint32_t)(i >> 1) & 1u, quit)) break;
@@ -261,54 +278,68 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       Place ld = seg;
       const int boxes = kKeys / maps.box, ahead = 32 / boxes;      // boxes of a tile; tiles whose pages the lanes look up at once
       bool ok = true;
-      int i = 0;
+      int i = 0, st = 0, asked = 0;                      // asked: units whose queries this warp requested
+      uint32_t turn = 1;                                 // parity of the wait for an empty stage: none is waited for the first time round
       for (int so = 0; i < n_all && ok; ++so) {          // segment by segment
         const int seg_n = min(n_all - i, ld.k.n - ld.t);
-        if (!keys && !load_queries(ld, so)) break;       // by the warp whose tiles are wanted later
         const int see_from = window_first(ld.len + quotient16(ld.qg * kQueries, a.group_inv), a.window);
         const int see_to = min(ld.len + quotient16(min(nq - 1, ld.qg * kQueries + kQueries - 1), a.group_inv), a.cap - 1);
         for (int g0 = 0; g0 < seg_n && ok; g0 += ahead) {
           const int t = tile_key(ld.k, ld.t + g0 + lane / boxes, kKeys) + lane % boxes * maps.box;
-          int page = -2, slot = 0;                       // the lane's box: -2, no row sees it, it is not loaded; -1: nor one without a page
+          int page = -2, x[3] = {0, 0, 0};               // the lane's box: -2, no row sees it, it is not loaded; -1: nor one without a page
           if (g0 + lane / boxes < seg_n && t <= see_to && (t + maps.box > see_from || t < a.n_sink)) {
-            const int e = (int)((unsigned int)t / (unsigned int)a.pool.page_size);
-            slot = t - e * a.pool.page_size;
+            const int e = (int)((unsigned int)t / (unsigned int)a.pool.page_size), slot = t - e * a.pool.page_size;
             page = max(-1, a.table[(long long)ld.b * a.width + e]);
             if (page >= a.pool.n_pages) page = -1;
+#pragma unroll
+            for (int d = 0; d < 3; ++d) x[d] = d + 1 == maps.slot_dim ? slot : d + 1 == maps.head_dim ? ld.kvh : page;
+          }
+          if (g0 == 0) {                                 // the queries first, the table is still on its way
+            if (maps.q_rows && keys) {
+              if (so >= 2 && !mbar_wait_warp(smem_u32(&q_free[so & 1]), (uint32_t)((so >> 1) - 1) & 1u, quit)) { ok = false; break; }
+              const uint32_t bar = smem_u32(&q_full[so & 1]), dst = tiles + S * C::kTile + (uint32_t)(so & 1) * C::kQ;
+              if (elect_one()) {
+                mbar_expect_tx(bar, C::kQ);
+#pragma unroll
+                for (int k = 0; k < C::SUB; ++k) {
+                  const int y[4] = {k * 64, 0, (a.first + ld.b) * a.c + ld.qg * maps.q_rows, ld.kvh};
+                  load_4d(dst + k * C::kQSub, &maps.q, y, bar);
+                }
+              }
+              __syncwarp();
+              ++asked;
+            } else if (!maps.q_rows && !keys && !load_queries(ld, so)) {
+              ok = false;
+              break;
+            }
           }
           const unsigned int all_bad = __ballot_sync(0xffffffffu, page == -1), all_here = __ballot_sync(0xffffffffu, page >= 0);
-          const unsigned int of_tile = boxes == 32 ? ~0u : (1u << boxes) - 1;
-          for (int g = 0; g < ahead && g0 + g < seg_n; ++g, ++i) {
-            const int st = i % S;
-            unsigned int bad = all_bad >> (g * boxes) & of_tile;
+          const unsigned int of_tile = (1u << boxes) - 1;
+          const int n = min(ahead, seg_n - g0);
+          for (int g = 0; g < n; ++g, ++i) {
             const unsigned int here = all_here >> (g * boxes) & of_tile;
-            if (i >= S && !mbar_wait_warp(smem_u32(&empty[st]), (uint32_t)(i / S - 1) & 1u, quit)) { ok = false; break; }
-            const uint32_t bar = smem_u32(&full[st]);
-            if (lane == 0) {
-              if (!keys) {
-                unsigned long long gone = 0;
-                for (; bad; bad &= bad - 1) gone |= (~0ull >> (64 - maps.box)) << ((__ffs(bad) - 1) * maps.box);
-                bad_keys[st][0] = (unsigned int)gone;
-                bad_keys[st][1] = (unsigned int)(gone >> 32);
-              }
-              mbar_expect_tx(bar, (uint32_t)(__popc(here) * maps.box) * (HD * 2u));
+            if (i >= S && !mbar_wait_warp(smem_u32(&empty[st]), turn, quit)) { ok = false; break; }
+            const uint32_t bar = smem_u32(&full[st]), dst = tiles + st * C::kTile + (keys ? 0u : C::kHalf);
+            if (!keys && lane == 0) {
+              unsigned long long gone = 0;
+              for (unsigned int bad = all_bad >> (g * boxes) & of_tile; bad; bad &= bad - 1) gone |= (~0ull >> (64 - maps.box)) << ((__ffs(bad) - 1) * maps.box);
+              bad_keys[st][0] = (unsigned int)gone;
+              bad_keys[st][1] = (unsigned int)(gone >> 32);
             }
+            if (lane == 0) mbar_expect_tx(bar, (uint32_t)(__popc(here) * maps.box) * (HD * 2u));
             __syncwarp();
-            const uint32_t dst = tiles + st * C::kTile + (keys ? 0u : C::kHalf);
-            for (unsigned int left = here; left; left &= left - 1) {
-              const int b = __ffs(left) - 1;
-              const int from = __shfl_sync(0xffffffffu, slot, g * boxes + b), in = __shfl_sync(0xffffffffu, page, g * boxes + b);
-              int x[4];
+            for (int b = 0; b < boxes; ++b) {
+              const int from = g * boxes + b;
+              const int at[4] = {0, __shfl_sync(0xffffffffu, x[0], from), __shfl_sync(0xffffffffu, x[1], from), __shfl_sync(0xffffffffu, x[2], from)};
+              if ((here >> b & 1u) && elect_one()) {
 #pragma unroll
-              for (int d = 1; d < 4; ++d) x[d] = d == maps.slot_dim ? from : d == maps.head_dim ? ld.kvh : in;
-              if (elect_one()) {
-#pragma unroll
-                for (int s = 0; s < C::SUB; ++s) {
-                  x[0] = s * 64;
-                  load_4d(dst + (uint32_t)(b * maps.box) * 128u + s * C::kSub, map, x, bar);
+                for (int k = 0; k < C::SUB; ++k) {
+                  const int y[4] = {k * 64, at[1], at[2], at[3]};
+                  load_4d(dst + (uint32_t)(b * maps.box) * 128u + k * C::kSub, map, y, bar);
                 }
               }
             }
+            if (++st == S) { st = 0; turn ^= 1u; }
           }
         }
         if (i < n_all) move_on<kKeys>(a, ld, seg_n);
@@ -317,6 +348,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         const unsigned long long t0 = clock64();
         for (int k = 0; k < S && k < i; ++k)
           while (!mbar_try(smem_u32(&full[k]), last_copy_parity(i, S, k)))
+            if ((unsigned long long)(clock64() - t0) > kSpinBudget / 4) break;
+        for (int k = 0; k < 2 && k < asked; ++k)
+          while (!mbar_try(smem_u32(&q_full[k]), last_copy_parity(asked, 2, k)))
             if ((unsigned long long)(clock64() - t0) > kSpinBudget / 4) break;
       }
     } else {
@@ -396,10 +430,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     // -------------------------------------------------------------------------------------------- softmax
     const int w = warp >> 2, row = tid & 127;
-    const uint32_t sc = tmem + w * 256 + ((uint32_t)(warp & 3) << 21);                          // this warp's 32 lanes
+    uint32_t sc = 0;
+    bool ok = tensor_memory(sc);
+    sc += w * 256 + ((uint32_t)(warp & 3) << 21);          // this warp's 32 lanes
     int i = w, done = 0, exchanges = 0;
     uint32_t odd_phase = 0;
-    bool ok = true;
     while (ok) {
       const int seg_n = min(n_mine - done, seg.k.n - seg.t);
       const int q0 = seg.qg * kQueries, q = q0 + row, qc = min(q, nq - 1), j = quotient16(qc, a.group_inv), h = seg.kvh * group + qc - j * group;
@@ -440,15 +475,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           add_product();
           if (!ok) break;
         }
+        const unsigned int bad0 = bad_keys[st][0], bad1 = bad_keys[st][1];
+        const bool masked = key0 + kKeys - 1 > p_first || (key0 < low_last && key0 + kKeys > a.n_sink) || (bad0 | bad1);
+        // Tiles that all rows see whole are most of them and have code of their own, without the jumps over what the others need.
+        auto tile = [&](auto kind) {
+        constexpr bool hard = decltype(kind)::value;
         float s[kKeys];
         tmem_ld64(sc, s);
         if (C::kApart) {
           tc_fence_before();
           mbar_arrive(smem_u32(&s_free[w]));
         }
-        const unsigned int bad0 = bad_keys[st][0], bad1 = bad_keys[st][1];
-        const bool masked = key0 + kKeys - 1 > p_first || (key0 < low_last && key0 + kKeys > a.n_sink) || (bad0 | bad1);
-        if (masked) {
+        if (hard) {
           // bit k: whether the row sees key key0 + k (all up to `to` but those between the sinks and the window), and has a page for it
           auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };     // bits 0 .. n - 1
           const unsigned long long see = below(pos + 1 - key0) & ~(below(low - key0) & ~below(a.n_sink - key0));
@@ -483,11 +521,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         l = fmaf(l, corr_now, sum[0].x + sum[0].y);
         if (C::kApart) {
           add_product();
-          if (!ok) break;
+          if (!ok) return;
         }
         // values that are not finite, in a tile that some row does not see whole (by TMA its unseen slots hold anything): those keys are
         // added row by row and taken out of the tile (a probability of zero would carry them to rows that do not see them)
-        if (masked) {
+        if (hard) {
           const uint32_t vb = base + st * C::kTile + C::kHalf;
           unsigned char *vg = base_g + (vb - base);
           unsigned int odd0 = 0, odd1 = 0;
@@ -504,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           if (odd1) atomicOr(&odd_keys[w][1], odd1);
           mbar_arrive(smem_u32(&odd_bar[w]));
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&odd_bar[w]), odd_phase, quit));
-          if (!ok) break;
+          if (!ok) return;
           odd_phase ^= 1u;
           odd0 = *(volatile unsigned int *)&odd_keys[w][0];
           odd1 = *(volatile unsigned int *)&odd_keys[w][1];
@@ -533,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
             }
             mbar_arrive(smem_u32(&odd_bar[w]));
             ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&odd_bar[w]), odd_phase, quit));
-            if (!ok) break;
+            if (!ok) return;
             odd_phase ^= 1u;
             for (int e = row; e < kKeys * PER; e += 128) {
               const int r = e / PER;
@@ -565,6 +603,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
+        };
+        if (masked) tile(std::true_type());
+        else tile(std::false_type());
+        if (!ok) break;
         mbar_arrive(smem_u32(&p_ready[w]));
       }
       if (ok) add_product();
@@ -607,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) tmem_dealloc(tmem, 512);
+  if (warp == 8) tmem_dealloc(*(volatile unsigned int *)&tmem_base_s, 512);
   if (tid == 0) a.status[blockIdx.x] = gave_up != 0;
 }
 
@@ -616,13 +658,13 @@ using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_
                                    const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 bool page_maps(const PagedAttnArgs &a, int hd, PageMaps *maps) {
   if (a.pool.page_size % 8) return false;
-  static EncodeTiledFn enc = nullptr;
-  if (!enc) {
+  static const EncodeTiledFn enc = [] {
     void *sym = nullptr;
     cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess) return false;
-    enc = (EncodeTiledFn)sym;
-  }
+    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess
+               ? (EncodeTiledFn)sym : (EncodeTiledFn) nullptr;
+  }();
+  if (!enc) return false;
   int box = 64;
   while (a.pool.page_size % box) box /= 2;
   struct Dim { int kind; cuuint64_t n; long long stride; } d[3] = {{0, (cuuint64_t)a.pool.page_size, a.slot_bytes}, {1, (cuuint64_t)a.pool.n_kv_heads, a.head_bytes},
@@ -640,6 +682,16 @@ bool page_maps(const PagedAttnArgs &a, int hd, PageMaps *maps) {
     if (d[i].kind == 0) { maps->slot_dim = i + 1; boxes[i + 1] = (cuuint32_t)box; }
     if (d[i].kind == 1) maps->head_dim = i + 1;
     if (d[i].kind == 2) maps->page_dim = i + 1;
+  }
+  // queries: a box holds the heads of a group for as many rows as make 128 (rows behind a sequence's are another's or zeros: nobody reads their results)
+  maps->q_rows = kQueries % a.group ? 0 : kQueries / a.group;
+  if (maps->q_rows) {
+    cuuint64_t qdim[4] = {(cuuint64_t)hd, (cuuint64_t)a.group, (cuuint64_t)a.batch * a.c, (cuuint64_t)a.pool.n_kv_heads};
+    cuuint64_t qstr[3] = {(cuuint64_t)hd * 2, (cuuint64_t)a.q_stride * 2, (cuuint64_t)a.group * hd * 2};
+    cuuint32_t qbox[4] = {64, (cuuint32_t)a.group, (cuuint32_t)maps->q_rows, 1};
+    if (qstr[1] >= (1ull << 40) ||
+        enc(&maps->q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(a.q), qdim, qstr, qbox, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) maps->q_rows = 0;
   }
   for (int v = 0; v < 2; ++v)
     if (enc(v ? &maps->v : &maps->k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, v ? a.pool.v : a.pool.k, gdim, gstr, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
