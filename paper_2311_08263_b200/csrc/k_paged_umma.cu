@@ -547,13 +547,17 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           odd0 = *(volatile unsigned int *)&odd_keys[w][0];
           odd1 = *(volatile unsigned int *)&odd_keys[w][1];
           if (odd0 | odd1) {
-#pragma unroll
-            for (int c = 0; c < HD / 2; ++c) { o[c].x *= corr_now; o[c].y *= corr_now; }
-            corr_now = 1.f;
+            bool scaled = false;                         // rows that see none of them are computed as ever: what they hold may be left over from anything
 #pragma unroll 1
             for (unsigned long long left = ((unsigned long long)odd1 << 32) | odd0; left; left &= left - 1) {
               const int kk = __ffsll((long long)left) - 1;
               if (!sees(pos, key0 + kk, a.window, a.n_sink)) continue;
+              if (!scaled) {
+#pragma unroll
+                for (int c = 0; c < HD / 2; ++c) { o[c].x *= corr_now; o[c].y *= corr_now; }
+                corr_now = 1.f;
+                scaled = true;
+              }
               float p = 0.f;
 #pragma unroll
               for (int k = 0; k < kKeys; ++k)

@@ -538,3 +538,188 @@ def test_questions_behind_one_prompt(dtype):
             own[2], own[1] = list(own[3]), []
     held = table[table >= 0].tolist()
     assert [held.count(p) for p in range(n_pages)] == refs.tolist()
+
+
+# ---------------------------------------------------------------------------------------------------------------- many queries per kv head
+def _widened(table, ps, cap):
+    """The table with columns of -1 for `cap` keys: which kernel a call takes follows from what its table may hold."""
+    more = -(-cap // ps) - table.shape[1]
+    return torch.cat([table, torch.full((table.shape[0], more), -1, dtype=torch.int32, device="cuda")], 1).contiguous() if more > 0 else table
+
+
+def _on_tcgen05(k, table, c, hq, window=0, n_sink=0):
+    """Whether the call asks for the scratch of the kernel with units of 128 queries: a status word for each of 148 CTAs, two parts of each."""
+    hkv, ps, hd = k.shape[1:]
+    want = 1024 + 148 * 2 * 128 * (hd + 2) * 4
+    return lib.load().fc_op_paged_attention_scratch_bytes(table.shape[0], c, hq, hkv, hd, lib.FC_BF16, table.shape[1], ps, window, n_sink) == want
+
+
+MANY = [
+    # hq, hkv, hd, c, page, layout, lens, window, sinks
+    (32, 4, 64, 16, 16, "hnd", EDGES, 0, 0),                                 # units of 128: queries, keys and values by TMA
+    (32, 4, 64, 16, 64, "nhd", EDGES, 0, 0),
+    (32, 4, 128, 16, 24, "turns", EDGES, 0, 0),
+    (32, 4, 128, 16, 8, "padded", EDGES, 0, 0),                              # eight boxes a tile
+    (16, 2, 128, 33, 128, "hnd", EDGES, 0, 0),                               # 264 queries, the last unit has eight
+    (16, 16, 64, 64, 40, "hnd", [300, 0, -1, 77], 0, 0),                     # one query per row: a box of 128 rows takes the next sequence's too
+    (12, 4, 64, 64, 16, "nhd", [300, 0, -1, 77, 1], 0, 0),                   # three: units begin inside rows
+    (26, 2, 128, 51, 1000, "hnd", [999, 998, 1000, 0], 0, 0),
+    (32, 4, 64, 16, 5, "hnd", EDGES, 0, 0),                                  # keys and values by copies
+    (32, 4, 128, 16, 1, "padded", EDGES, 0, 0),
+    (20, 4, 128, 64, 20, "turns", [200, 1, -1, 77], 0, 0),
+    (32, 4, 64, 16, 16, "hnd", [900] + EDGES, 130, 5),
+    (32, 4, 128, 16, 48, "nhd", [900] + EDGES, 1, 0),
+    (16, 2, 128, 64, 20, "hnd", [700, 3, 65], 100, 200),
+    (8, 4, 64, 64, 8, "hnd", [700, 250, 5], 33, 0),
+]
+
+
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_many_queries(case):
+    hq, hkv, hd, c, ps, order, lens, window, n_sink = MANY[case]
+    k, v, table, kv_len = _cache(lens, c, hkv, hd, ps, torch.bfloat16, order, 200 + case, window, n_sink)
+    rep = -(-320 // (len(lens) * hkv)) if window else 1                      # under a window the table's bound says little: the same sequences again
+    table = _widened(table, ps, 40000)
+    B = len(lens)
+    assert _on_tcgen05(k, table.repeat(rep, 1), c, hq, window, n_sink)
+    wide = _queries(B * c, hq * hd + 8, torch.bfloat16, case)
+    for q in (wide[:, 8:], wide[:, 8:].contiguous()):
+        want = ref.attention(q, k, v, table, kv_len, c, hq, window, n_sink)
+        q = wide.repeat(rep, 1)[:, 8:] if q.stride(0) > q.shape[1] else q.repeat(rep, 1)
+        out = engine.fc_op_paged_attention(q, k, v, table.repeat(rep, 1), kv_len.repeat(rep), c, hq, window=window, n_sink=n_sink)
+        _close(out, *(x.repeat(rep, 1, 1) for x in want))
+
+
+@pytest.mark.parametrize("hd,ps", [(64, 16), (64, 20), (128, 64), (128, 9)])
+def test_many_queries_and_long_lines(hd, ps):
+    """Some forty tiles per CTA and several units of each: every stage of the rings is used many times, units end and begin inside a piece."""
+    hq, hkv, c, lens = 64, 8, 16, [3000, 2999, 64, 0, 1500, 1, 700, 2048, 127, 63, 2400, 5, -1, 1900, 1000, 2500]
+    gen = torch.Generator().manual_seed(hd)
+    table, n_pages = _dealt(lens, c, ps, gen)
+    k, v = (torch.randn(n_pages, hkv, ps, hd, generator=gen).to(torch.bfloat16).cuda() for _ in range(2))
+    table, kv_len = table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+    q = _queries(len(lens) * c, hq * hd, torch.bfloat16, 1)
+    assert _on_tcgen05(k, table, c, hq)
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq)
+    _close(out, *ref.attention(q, k, v, table, kv_len, c, hq))
+
+
+@pytest.mark.parametrize("hd,ps", [(64, 16), (64, 5), (128, 24), (128, 7)])
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (6, 2)])
+def test_many_queries_later_rows_do_not_reach_earlier_ones(hd, ps, window, n_sink):
+    hq, hkv, c, lens = 64, 4, 12, [150, 3, 0, 63, 64, 500] * 14              # 192 queries per kv head
+    k, v, table, kv_len = _cache(lens, c, hkv, hd, ps, torch.bfloat16, "hnd", 5, window, n_sink)
+    table = _widened(table, ps, 5000)
+    q = _queries(len(lens) * c, hq * hd, torch.bfloat16, 6)
+    good = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq, window=window, n_sink=n_sink).view(len(lens), c, hq, hd)
+    assert _on_tcgen05(k, table, c, hq, window, n_sink)
+    tab = table.tolist()
+    for bad in (math.nan, math.inf, -math.inf):
+        for at in (4, 11):
+            k2, v2 = k.clone(), v.clone()
+            for b, n in enumerate(lens):
+                page, slot = tab[b][(n + at) // ps], (n + at) % ps
+                v2[page, :, slot, ::3] = bad
+                if bad != bad:
+                    k2[page, :, slot, 5] = bad
+            out = engine.fc_op_paged_attention(q, k2, v2, table, kv_len, c, hq, window=window, n_sink=n_sink).view(len(lens), c, hq, hd)
+            for j in range(c):
+                for b, n in enumerate(lens):
+                    if at + n not in ref.visible(n + j, window, n_sink):
+                        assert torch.equal(out[b, j], good[b, j]), (b, j)
+                    elif bad != bad:
+                        assert out[b, j].isnan().all()
+                    else:
+                        assert (out[b, j, :, ::3] == bad).all() and out[b, j, :, 1::3].isfinite().all()
+
+
+@pytest.mark.parametrize("hd,ps", [(64, 16), (128, 16), (64, 20), (128, 64)])
+def test_many_queries_and_bad_pages(hd, ps):
+    hq, hkv, c, lens = 32, 4, 16, [390, 400, 400, 140, 0, 60]
+    k, v, table, kv_len = _cache(lens, c, hkv, hd, ps, torch.bfloat16, "hnd", 8)
+    table[0, 400 // ps] = -1                                                 # in the window: the rows from there on, where a page begins there
+    table[1, 5] = k.shape[0]
+    table[2, 0] = 2 ** 31 - 1
+    table[3, 160 // ps + 1] = -5                                             # no row sees it
+    table[5, (60 + 8) // ps] = -1
+    table = _widened(table, ps, 40000)
+    q = _queries(len(lens) * c, hq * hd, torch.bfloat16, 6)
+    assert _on_tcgen05(k, table, c, hq)
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq)
+    want, tol = ref.attention(q, k, v, table, kv_len, c, hq)
+    rows = want.view(len(lens), c, -1).isnan().all(2).sum(1).tolist()
+    assert rows[:3] == [c if ps == 64 else 6, c, c] and rows[3:] == [0, 0, c if ps == 20 else 12]
+    assert not want.view(len(lens), -1)[3:5].isnan().any()
+    _close(out, want, tol)
+
+
+def test_many_queries_and_offsets_beyond_32_bits():
+    hkv, hd, ps, hq, c, n = 8, 128, 64, 64, 16, 230
+    n_pages = 2 ** 31 // (hkv * hd * ps) + 40
+    k, v = (torch.empty(n_pages, hkv, ps, hd, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 3, n_pages - 2]], dtype=torch.int32).cuda()
+    for x in (k, v):
+        for p in table[0].tolist():
+            x[p] = torch.randn(hkv, ps, hd, generator=torch.Generator().manual_seed(p)).to(torch.bfloat16).cuda()
+    kv_len = torch.tensor([n], dtype=torch.int32).cuda()
+    wide = _widened(table, ps, 40000)
+    q = _queries(c, hq * hd, torch.bfloat16, 3)
+    assert _on_tcgen05(k, wide, c, hq)
+    out = engine.fc_op_paged_attention(q, k, v, wide, kv_len, c, hq)
+    few = table[0].long()
+    _close(out, *ref.attention(q, k[few], v[few], torch.tensor([[0, 1, 2, 3]]), kv_len, c, hq))
+
+
+def test_many_queries_captured_and_on_two_streams():
+    """The same bits from calls on two streams at once and from a graph that is replayed with other lengths, as from calls one by one."""
+    cases = []
+    for i, (hq, hkv, hd, ps) in enumerate([(32, 4, 64, 16), (64, 8, 128, 20)]):
+        lens = [1200, 40, 900, 0, 641, 64, 300, 2]
+        k, v, table, kv_len = _cache(lens, 16, hkv, hd, ps, torch.bfloat16, "hnd", i)
+        k, v = (torch.nan_to_num(x) for x in (k, v))
+        cases.append((_queries(len(lens) * 16, hq * hd, torch.bfloat16, i), k, v, _widened(table, ps, 40000), kv_len, 16, hq))
+        assert _on_tcgen05(k, cases[-1][3], 16, hq)
+    first = [engine.fc_op_paged_attention(*a) for a in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for s, a in zip(streams, cases):
+            with torch.cuda.stream(s):
+                got.append(engine.fc_op_paged_attention(*a))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, first[i % 2]) for i, x in enumerate(got))
+    graphs, outs = [], []
+    for a in cases:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(engine.fc_op_paged_attention(*a))
+    shorter = [a[4] // 3 for a in cases]
+    want = [engine.fc_op_paged_attention(*a[:4], n, *a[5:]) for a, n in zip(cases, shorter)]
+    for a, n in zip(cases, shorter):
+        a[4].copy_(n)
+    torch.cuda.synchronize()
+    for _ in range(3):                                                       # both graphs at once
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(outs, want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,c", [(2, 1), (8, 2), (16, 8)])
+def test_tables_of_more_tiles_than_one_launch_counts(dtype, hq, c):
+    """Pages of 2^20 slots, 2^10 of them to a sequence: tiles are counted in 31 bits, so that the sequences are dealt out to several launches."""
+    hkv, hd, ps, B = 1, 64, 1 << 20, 400
+    k, v = _pools(2, hkv, ps, hd, DT[dtype])
+    for x in (k, v):
+        x[:, :, :260] = torch.randn(2, hkv, 260, hd, generator=torch.Generator().manual_seed(2)).to(DT[dtype]).cuda()
+    table = torch.full((B, 1 << 10), -1, dtype=torch.int32).cuda()
+    table[:, 0] = torch.arange(B, dtype=torch.int32).cuda() % 2
+    kv_len = torch.tensor([(7 * b) % 250 - 1 for b in range(B)], dtype=torch.int32).cuda()
+    q = _queries(B * c, hq * hd, DT[dtype], 1)
+    if dtype == "bf16" and hq * c > 32:
+        assert _on_tcgen05(k, table, c, hq)
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq)
+    _close(out, *ref.attention(q, k, v, table, kv_len, c, hq))
