@@ -182,13 +182,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
         odd = __reduce_or_sync(0xffffffffu, odd);
         if (odd) {
 #pragma unroll
-          for (int n = 0; n < QN; ++n) {
+          for (int n = 0; n < QN; ++n)
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+            for (int x = 0; x < 2; ++x) {                // rows that see none of them are computed as ever
+              bool hit = false;
+              for (unsigned int left = odd; left; left &= left - 1) hit |= sees(pos[n][x], key0 + __ffs(left) - 1, a.window, a.n_sink);
+              if (!hit) continue;
 #pragma unroll
-              for (int x = 0; x < 4; ++x) o[n][d][x] *= corr[n][x & 1];
-            corr[n][0] = corr[n][1] = 1.f;
-          }
+              for (int d = 0; d < DB; ++d) {
+                o[n][d][x] *= corr[n][x];
+                o[n][d][x + 2] *= corr[n][x];
+              }
+              corr[n][x] = 1.f;
+            }
           for (unsigned int left = odd; left; left &= left - 1) {
             const int kk = __ffs(left) - 1;
 #pragma unroll

@@ -723,3 +723,20 @@ def test_tables_of_more_tiles_than_one_launch_counts(dtype, hq, c):
         assert _on_tcgen05(k, table, c, hq)
     out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq)
     _close(out, *ref.attention(q, k, v, table, kv_len, c, hq))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd,ps,c", [(64, 16, 8), (128, 24, 16), (32, 5, 3), (128, 16, 2)])
+def test_rows_of_long_lines_keep_their_bits(dtype, hd, ps, c):
+    """A value that is not finite in the last key of the window: earlier rows have the same bits where it meets sums of earlier tiles too."""
+    hq, hkv, lens = 4, 4, [701, 640, 655, 3, 320] * 8
+    k, v, table, kv_len = _cache(lens, c, hkv, hd, ps, DT[dtype], "hnd", 7)
+    q = _queries(len(lens) * c, hq * hd, DT[dtype], 6)
+    good = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq).view(len(lens), c, hq, hd)
+    tab = table.tolist()
+    for b, n in enumerate(lens):
+        v[tab[b][(n + c - 1) // ps], :, (n + c - 1) % ps, ::3] = math.inf
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq).view(len(lens), c, hq, hd)
+    assert torch.equal(out[:, :-1], good[:, :-1]) and (out[:, -1, :, ::3] == math.inf).all()
+    fine = torch.arange(hd).cuda() % 3 != 0
+    assert torch.allclose(out[:, -1][..., fine], good[:, -1][..., fine], rtol=0, atol=1e-5)
