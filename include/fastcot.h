@@ -287,7 +287,7 @@ int fc_op_window_attention_noalloc(const void *q, const void *kcache, const void
  * max_seq slots per page and a page per sequence.
  * Sequences are rows of a table, device int32 [n_seqs, table_width]: entry i is the page of positions i * page_size ..; -1: none.
  * kv_len, device int32 [n_seqs]: committed tokens; -1: the row holds no sequence.  refs, device int32 [n_pages]: table entries that
- * hold the page; 0: free.  The caller owns all of it and starts with tables of -1, kv_len -1, refs 0.
+ * hold the page; 0: free.  No page stands twice in a row.  The caller owns all of it and starts with tables of -1, kv_len -1, refs 0.
  *
  * Unlike the other operations these calls only enqueue work on cuda_stream (no wait, no allocation, no copy from host memory that
  * the caller has to keep), so they can be captured; lengths, tables and reference counts are read on the device when the work runs.  The
@@ -315,7 +315,8 @@ int fc_op_paged_store(const fc_pages *pages, int32_t layer, const int32_t *table
  * and values are in their slots already.  q: [batch * c] rows of n_heads * head_dim in the pool's type, q_stride elements apart; out: fp32
  * [batch * c, n_heads * head_dim].  Rows of a table row without a sequence are 0.  A row that sees a key whose page is not in the
  * pool, or lies beyond the table, is NaN; pages that no row sees may be missing.  Keys and values that a row does not see do not reach
- * it, whatever they hold.  Results do not depend on the order in which the work runs.
+ * it, whatever they hold.  Scores of minus infinity weigh nothing; a row that has no other is NaN.  Results do not depend on the order in which
+ * the work runs.
  * c <= 64, n_heads <= 512 (else, and for tables of some ten million positions and many heads, FC_ERR_CAPACITY); q, out 16-byte aligned, q_stride a
  * multiple of 16 bytes; scratch: device, 256-byte aligned, at least ..._scratch_bytes(...) bytes for these arguments, whatever the lengths; what it holds
  * before and after means nothing.  That function returns 0 for what is refused, and 256 where the call uses no scratch (which may be NULL then). */

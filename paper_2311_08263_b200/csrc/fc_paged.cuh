@@ -109,9 +109,9 @@ __device__ __forceinline__ Place find_place(const PagedAttnArgs &a, int f) {
   return p;
 }
 
-// Result of a query: un-normalised sums over `den`.  A row that sees nothing is 0, one beyond the table NaN.
+// Result of a query: un-normalised sums over `den`.  A row beyond the table is NaN, and so is one whose scores are all minus infinity (zeros over zero).
 __device__ __forceinline__ float result_scale(const PagedAttnArgs &a, int pos, float den) {
-  return pos >= a.cap ? quiet_nan() : den == 0.f ? 0.f : 1.0f / den;
+  return pos >= a.cap ? quiet_nan() : 1.0f / den;
 }
 
 // Byte offset of 16-byte piece `ch` of key `r` in a tile of KEYS rows of ROW bytes: sub-tiles of 128 bytes a row, pieces permuted so that eight rows at

@@ -328,6 +328,12 @@ def _lengths(kv_len: torch.Tensor, n: int, device: int) -> int:
     return _ints("kv_len", kv_len, 1, device)
 
 
+def _rows(x: torch.Tensor):
+    """Strides of a matrix; that of a single row says nothing."""
+    row, elem = x.stride()
+    return (row, elem) if x.shape[0] > 1 else (x.shape[1], elem)
+
+
 def _list(ids):
     return (C.c_int32 * len(ids))(*ids)
 
@@ -356,7 +362,7 @@ def fc_op_paged_store(qkv: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table
     pool, device = _pool(k, v, 4), k.get_device()
     tab = _ints("table", table, 2, device)
     B, width = table.shape
-    row, elem = qkv.stride()
+    row, elem = _rows(qkv)
     if (qkv.dtype is not torch.float32 or qkv.shape != (B * c, (n_heads + 2 * pool.n_kv_heads) * pool.head_dim) or elem != 1
             or qkv.get_device() != device):
         raise ValueError("qkv: fp32 [B * c, (n_heads + 2 n_kv_heads) * head size] with adjacent elements, on the pool's device")
@@ -374,7 +380,7 @@ def fc_op_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tab
     tab = _ints("table", table, 2, device)
     B, width = table.shape
     hd = pool.head_dim
-    row, elem = q.stride()
+    row, elem = _rows(q)
     if q.dtype is not k.dtype or q.shape != (B * c, n_heads * hd) or elem != 1 or q.get_device() != device:
         raise ValueError("q: [B * c, n_heads * head size] in the pool's type with adjacent elements, on the pool's device")
     nbytes = _scratch_bytes("fc_op_paged_attention_scratch_bytes", B, c, n_heads, pool.n_kv_heads, hd, pool.dtype, width, pool.page_size, window, n_sink)

@@ -740,3 +740,38 @@ def test_rows_of_long_lines_keep_their_bits(dtype, hd, ps, c):
     assert torch.equal(out[:, :-1], good[:, :-1]) and (out[:, -1, :, ::3] == math.inf).all()
     fine = torch.arange(hd).cuda() % 3 != 0
     assert torch.allclose(out[:, -1][..., fine], good[:, -1][..., fine], rtol=0, atol=1e-5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,c,n,width", [(2, 1, 40, 3), (2, 1, 9000, 600), (16, 2, 300, 30), (8, 16, 300, 2500)])
+def test_infinite_scores(dtype, hq, c, n, width):
+    """Scores of minus infinity weigh nothing; a row that sees no other is NaN, and so is one that sees plus infinity."""
+    hkv, hd, ps = 2, 64, 16
+    k, v, table, kv_len = _cache([n] * 3, c, hkv, hd, ps, DT[dtype], "hnd", 3)
+    table = _widened(table, ps, width * ps)
+    q = _queries(3 * c, hq * hd, DT[dtype], 1).abs() + 0.1
+    live = (n + c - 1) // ps + 1
+    fine = k.clone()
+    for page in table[0, :live].tolist():                                    # every key of the first sequence
+        k[page, :, :, 3] = -math.inf
+    k[table[1, 0].item(), :, 5, 3] = -math.inf                                # one key of the second
+    k[table[2, 0].item(), 1, 5, 3] = math.inf                                # one key of one head of the third
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq).view(3, c, hkv, -1)
+    want, tol = ref.attention(q, k, v, table, kv_len, c, hq)
+    want, tol = want.view(3, c, hkv, -1), tol.view(3, c, hkv, -1)
+    assert want[0].isnan().all() and want[2, :, 1].isnan().all() and not want[1].isnan().any() and not want[2, :, 0].isnan().any()
+    assert torch.equal(out.isnan().cpu(), want.isnan())
+    # the bound from finite scores, twice, because the other keys weigh more without that one
+    _, tol = ref.attention(q, fine, v, table, kv_len, c, hq)
+    assert ((out[1].double().cpu() - want[1]).abs() <= 2 * tol.view(3, c, hkv, -1)[1]).all()
+
+
+def test_a_single_row_may_have_any_stride():
+    k, v, table, kv_len = _cache([20], 1, 2, 64, 16, torch.float32, "hnd", 3)
+    q = _queries(1, 4 * 64, torch.float32, 0)
+    odd = q.as_strided((1, 256), (1, 1))
+    a, b = (engine.fc_op_paged_attention(x, k, v, table, kv_len, 1, 4) for x in (q, odd))
+    assert torch.equal(a, b)
+    qkv = torch.randn(1, 8 * 64, generator=torch.Generator().manual_seed(1)).cuda()
+    a, b = (engine.fc_op_paged_store(x, k, v, table, kv_len, 1, 4, 1e4) for x in (qkv, qkv.as_strided((1, 512), (3, 1))))
+    assert torch.equal(a, b)
