@@ -91,11 +91,9 @@ __device__ __forceinline__ void tmem_ld64(uint32_t taddr, float *v) {
 #pragma unroll
   for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 
 // Two fp32 operations in one instruction.
@@ -471,10 +469,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[w]), turn, quit) && mbar_wait(smem_u32(&v_full[st]), (uint32_t)(i / S) & 1u, quit));
         if (!ok) break;
         tc_fence_after();
-        if (!C::kApart) {                                // scores over parts: the product in front of them is there
-          add_product();
-          if (!ok) break;
-        }
+        // Before the scores are loaded: at hd 128 they lie over parts that the product still reads, and so the registers hold one or the other (behind the
+        // exponentials, at hd 64, 38.2 us against 36.8 on 16 sequences of 16 rows; in front of the wait above 37.4).
+        add_product();
+        if (!ok) break;
         const unsigned int bad0 = bad_keys[st][0], bad1 = bad_keys[st][1];
         const bool masked = key0 + kKeys - 1 > p_first || (key0 < low_last && key0 + kKeys > a.n_sink) || (bad0 | bad1);
         // Tiles that all rows see whole are most of them and have code of their own, without the jumps over what the others need.
@@ -507,25 +505,24 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
           for (int x = 0; x < 4; ++x) mx[x] = k + 4 + x < kKeys ? fmaxf(fmaxf(mx[x], s[k + x]), s[k + 4 + x]) : fmaxf(mx[x], s[k + x]);
         mx[0] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         float corr_now = mx[0] == m ? 1.f : ex2((m - mx[0]) * sl2);                            // first tile: 2^-inf = 0
+        const float l_corr = corr_now;
         m = mx[0];
         const float mb = m == -INFINITY ? 0.f : -m * sl2;
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        auto exponentials = [&](int from) {              // of 16 scores
 #pragma unroll
-        for (int k = 0; k < kKeys; k += 2) {
-          const float2 x = fma2(make_float2(s[k], s[k + 1]), make_float2(sl2, sl2), make_float2(mb, mb));
-          s[k] = ex2(x.x);
-          s[k + 1] = ex2(x.y);
-          sum[(k >> 1) & 1] = add2(sum[(k >> 1) & 1], make_float2(s[k], s[k + 1]));
-        }
-        sum[0] = add2(sum[0], sum[1]);
-        l = fmaf(l, corr_now, sum[0].x + sum[0].y);
-        if (C::kApart) {
-          add_product();
-          if (!ok) return;
-        }
+          for (int k = from; k < from + 16; k += 2) {
+            const float2 x = fma2(make_float2(s[k], s[k + 1]), make_float2(sl2, sl2), make_float2(mb, mb));
+            s[k] = ex2(x.x);
+            s[k + 1] = ex2(x.y);
+            sum[(k >> 1) & 1] = add2(sum[(k >> 1) & 1], make_float2(s[k], s[k + 1]));
+          }
+        };
         // values that are not finite, in a tile that some row does not see whole (by TMA its unseen slots hold anything): those keys are
         // added row by row and taken out of the tile (a probability of zero would carry them to rows that do not see them)
         if (hard) {
+#pragma unroll
+          for (int from = 0; from < kKeys; from += 16) exponentials(from);
           const uint32_t vb = base + st * C::kTile + C::kHalf;
           unsigned char *vg = base_g + (vb - base);
           unsigned int odd0 = 0, odd1 = 0;
@@ -587,15 +584,16 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         }
         corr = corr_now;
         last = i;
-        // ---- probabilities in three parts, cut off (8 bits each)
+        // ---- probabilities in three parts, cut off (8 bits each), 16 keys at a time: what is between exponentials overlaps with them
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int from = 0; from < kKeys; from += 16) {
+          if (!hard) exponentials(from);
 #pragma unroll
           for (int part = 0; part < 3; ++part) {
-            uint32_t r[16];
+            uint32_t r[8];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              float &p0 = s[half * 32 + 2 * k], &p1 = s[half * 32 + 2 * k + 1];
+            for (int k = 0; k < 8; ++k) {
+              float &p0 = s[from + 2 * k], &p1 = s[from + 2 * k + 1];
               r[k] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
               if (part < 2) {
                 const float2 x = fma2(make_float2(low_half(r[k]), high_half(r[k])), make_float2(-1.f, -1.f), make_float2(p0, p1));
@@ -603,8 +601,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
                 p1 = x.y;
               }
             }
-            tmem_st16(sc + C::kP + part * 32 + half * 16, r);
+            tmem_st8(sc + C::kP + part * 32 + from / 2, r);
           }
+        }
+        sum[0] = add2(sum[0], sum[1]);
+        l = fmaf(l, l_corr, sum[0].x + sum[0].y);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         };
