@@ -22,7 +22,6 @@ namespace {
 
 constexpr int kKeys = kUmmaKeys, kQueries = kUmmaQueries;
 constexpr int kThreads = 384;
-constexpr int kSoftRegs = 224, kLoadRegs = 56;           // registers a thread: 256 x 224 + 128 x 56 = 384 x 168, what the launch holds
 constexpr int kCopyWarps = 2;                            // that load tiles where TMA does not
 
 template <int HD>
@@ -37,6 +36,10 @@ struct UmmaCfg {
   static constexpr bool kApart = HD == 64;
   static constexpr uint32_t kP = kApart ? 64 : 0, kO = kApart ? 160 : 128;
   static constexpr size_t kSmem = 1024 + (size_t)S * kTile + 2 * kQ + kExchange;
+  // Registers a thread, of softmax and of the third group: 384 x 168 in all, what the launch holds.  (hd 64, 16 sequences of 16 rows: 224 and 56 35.7 us,
+  // 208 and 88 35.0, 200 and 104 36.3; hd 128, 8 x 8 x 128 queries over 2000 keys: 45.2, 49.2 with 208 and 88.)
+  static constexpr int kSoftRegs = HD == 64 ? 208 : 224, kLoadRegs = HD == 64 ? 88 : 56;
+  static_assert(256 * kSoftRegs + 128 * kLoadRegs == kThreads * 168, "");
 };
 
 // 16-byte piece `ch` of row `r` in a tile of `rows` rows: rows of 128 bytes, the 128-byte swizzle of the MMA's operands.
@@ -175,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kLoadRegs));
     // Barriers of the tiles: what TMA or copies complete, and what the products free.  A warp that gives up a wait leaves its loop.
     auto drain = [&](int k) {                            // what this warp issued has completed, its arrivals are made: then memory may be given up
       if (elect_one()) umma_commit(smem_u32(&drained[k]));
@@ -425,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       if (ok) landed();
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftRegs));
     // -------------------------------------------------------------------------------------------- softmax
     const int w = warp >> 2, row = tid & 127;
     uint32_t sc = 0;
@@ -713,7 +716,7 @@ cudaError_t launch(const PageMaps &maps, const PagedAttnArgs &a, cudaStream_t st
     // the register split is only there to be had if the launch holds what it adds up to
     cudaFuncAttributes at;
     if (cudaError_t e = cudaFuncGetAttributes(&at, paged_umma_kernel<HD, TMA>)) return e;
-    if (at.numRegs * kThreads < 256 * kSoftRegs + 128 * kLoadRegs) return cudaErrorInvalidConfiguration;
+    if (at.numRegs * kThreads < 256 * C::kSoftRegs + 128 * C::kLoadRegs) return cudaErrorInvalidConfiguration;
     if (cudaError_t e = allow_smem(paged_umma_kernel<HD, TMA>, C::kSmem, done)) return e;
   }
   return by_lines(a, kKeys, [&](const PagedAttnArgs &part) {
