@@ -142,24 +142,25 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
   const uint32_t q_base = base + S * C::kTile;
   float4 *exchange = reinterpret_cast<float4 *>(base_g + S * C::kTile + 2 * C::kQ);      // piece c4 of row r at r * 16 + (c4 ^ (r & 15))
 
-  if (tid == 0) {
-    for (int i = 0; i < S; ++i) {
-      mbar_init(smem_u32(&k_full[i]), 1); mbar_init(smem_u32(&v_full[i]), 1); mbar_init(smem_u32(&k_empty[i]), 1); mbar_init(smem_u32(&v_empty[i]), 1);
-    }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&q_full[i]), 1); mbar_init(smem_u32(&q_free[i]), 1); mbar_init(smem_u32(&s_ready[i]), 1); mbar_init(smem_u32(&o_ready[i]), 1);
-      mbar_init(smem_u32(&s_free[i]), 128); mbar_init(smem_u32(&p_ready[i]), 128); mbar_init(smem_u32(&odd_bar[i]), 128); mbar_init(smem_u32(&drained[i]), 1);
-      odd_keys[i][0] = odd_keys[i][1] = 0u;
-    }
+  if (tid < S) {
+    mbar_init(smem_u32(&k_full[tid]), 1); mbar_init(smem_u32(&v_full[tid]), 1); mbar_init(smem_u32(&k_empty[tid]), 1); mbar_init(smem_u32(&v_empty[tid]), 1);
+    fence_barrier_init();
+  } else if (tid >= 32 && tid < 34) {
+    const int i = tid - 32;
+    mbar_init(smem_u32(&q_full[i]), 1); mbar_init(smem_u32(&q_free[i]), 1); mbar_init(smem_u32(&s_ready[i]), 1); mbar_init(smem_u32(&o_ready[i]), 1);
+    mbar_init(smem_u32(&s_free[i]), 128); mbar_init(smem_u32(&p_ready[i]), 128); mbar_init(smem_u32(&odd_bar[i]), 128); mbar_init(smem_u32(&drained[i]), 1);
+    odd_keys[i][0] = odd_keys[i][1] = 0u;
+    fence_barrier_init();
+  } else if (tid == 64) {
     mbar_init(smem_u32(&ex_full), 128); mbar_init(smem_u32(&ex_free), 128); mbar_init(smem_u32(&tmem_here), 1);
     gave_up = 0;
     fence_barrier_init();
-    fence_proxy_async();
   }
-  __syncthreads();
+  fence_proxy_async();
   Place seg;
   int n_mine;
   if (!my_piece<kKeys, true>(a, blockIdx.x, kSms, seg, n_mine)) return;
+  __syncthreads();
   // tensor memory comes while the loads begin; whoever uses it waits for it
   if (warp == 8) {
     tmem_alloc(smem_u32(&tmem_base_s), 512);
