@@ -279,14 +279,13 @@ __global__ void __launch_bounds__(kCombine) paged_combine_kernel(const __grid_co
   UnitParts w = {0, -1};
   if (k.n > 0) {
     w = unit_parts(begin, k.n, chunk);
-    if (w.first == w.last && !a.status) return;          // written by its one worker
+    // written by its one worker; but one block always waits, so that this kernel does not end before the line does
+    if (w.first == w.last && !a.status && (blockIdx.x | blockIdx.y)) return;
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   bool lost = false;                                     // a CTA that gave up a wait left nothing that counts
-  if (a.status) {
-    lost = __syncthreads_or(tid <= w.last - w.first && __ldcg(a.status + w.first + tid) != 0u);
-    if (w.first == w.last && !lost) return;
-  }
+  if (a.status) lost = __syncthreads_or(tid <= w.last - w.first && __ldcg(a.status + w.first + tid) != 0u);
+  if (w.first == w.last && !lost) return;
   const float sl2 = rsqrtf((float)HD) * 1.4426950408889634f;
   int groups = 1;
   while (groups * 2 * items <= kCombine) groups *= 2;

@@ -775,3 +775,19 @@ def test_a_single_row_may_have_any_stride():
     qkv = torch.randn(1, 8 * 64, generator=torch.Generator().manual_seed(1)).cuda()
     a, b = (engine.fc_op_paged_store(x, k, v, table, kv_len, 1, 4, 1e4) for x in (qkv, qkv.as_strided((1, 512), (3, 1))))
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_what_follows_a_line_of_whole_units_reads_its_results(dtype):
+    """As many units of one length as there are workers: each is whole, nothing is joined, and the next kernel of the stream finds them done."""
+    B, hkv, hd, ps, n = 37, 32, 64, 64, 2047
+    k, v = (torch.randn(n // ps + 1, hkv, ps, hd, generator=torch.Generator().manual_seed(3)).to(DT[dtype]).cuda() for _ in range(2))
+    table = torch.arange(n // ps + 1, dtype=torch.int32).cuda().repeat(B, 1)                    # one prompt, read by all
+    kv_len = torch.full((B,), n, dtype=torch.int32).cuda()
+    q = _queries(B, hkv * hd, DT[dtype], 1)
+    for _ in range(5):
+        torch.full((B, hkv * hd), math.nan, device="cuda")                                       # the memory that the result gets
+        out = engine.fc_op_paged_attention(q, k, v, table, kv_len, 1, hkv)
+        copy = out + 0
+        torch.cuda.synchronize()
+        assert torch.equal(copy, out) and out.isfinite().all()
