@@ -317,6 +317,7 @@ int fc_op_paged_store(const fc_pages *pages, int32_t layer, const int32_t *table
  * pool, or lies beyond the table, is NaN; pages that no row sees may be missing.  Keys and values that a row does not see do not reach
  * it, whatever they hold.  Scores of minus infinity weigh nothing; a row that has no other is NaN.  Results do not depend on the order in which
  * the work runs.
+ * (The waits inside its kernels are bounded; should one run out, which no argument or content causes, the rows that it concerns are NaN.)
  * c <= 64, n_heads <= 512 (else, and for tables of some ten million positions and many heads, FC_ERR_CAPACITY); q, out 16-byte aligned, q_stride a
  * multiple of 16 bytes; scratch: device, 256-byte aligned, at least ..._scratch_bytes(...) bytes for these arguments, whatever the lengths; what it holds
  * before and after means nothing.  That function returns 0 for what is refused, and 256 where the call uses no scratch (which may be NULL then). */

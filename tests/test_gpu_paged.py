@@ -791,3 +791,27 @@ def test_what_follows_a_line_of_whole_units_reads_its_results(dtype):
         copy = out + 0
         torch.cuda.synchronize()
         assert torch.equal(copy, out) and out.isfinite().all()
+
+
+def test_copies_beyond_32_bits():
+    """Copy on write between pages, and compaction of pages, that lie more than 2^32 bytes and 2^31 elements into a layer."""
+    hkv, hd, ps, layers = 8, 128, 64, 2
+    n = 2 ** 31 // (hkv * hd * ps) + 40
+    k, v = (torch.empty(layers, n, hkv, ps, hd, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    fill = {p: torch.randn(2, layers, hkv, ps, hd, generator=torch.Generator().manual_seed(p)).to(torch.bfloat16).cuda() for p in (0, n - 3, n - 2)}
+    for p, x in fill.items():
+        k[:, p], v[:, p] = x[0], x[1]
+    table = torch.tensor([[n - 2, -1], [n - 2, -1], [0, n - 3]], dtype=torch.int32).cuda()
+    kv_len = torch.tensor([10, 10, 70], dtype=torch.int32).cuda()
+    refs = torch.ones(n, dtype=torch.int32).cuda()
+    refs[n - 2], refs[n - 1] = 2, 0                                          # the only free page is the last
+    assert engine.fc_op_pages_reserve(k, v, table, kv_len, refs, 1).tolist() == [1, 1, 1]
+    assert table.tolist() == [[n - 1, -1], [n - 2, -1], [0, n - 3]] and refs[n - 3:].tolist() == [1, 1, 1]
+    for x, y in ((k, fill[n - 2][0]), (v, fill[n - 2][1])):
+        assert torch.equal(x[:, n - 1], y)
+    refs.zero_()
+    refs[0], refs[n - 3:] = 1, 1
+    assert engine.fc_op_pages_compact(k, v, table, refs).tolist() == [4]
+    assert table.tolist() == [[3, -1], [2, -1], [0, 1]] and refs[:4].tolist() == [1] * 4 and refs[4:].sum() == 0
+    for p, at in ((0, 0), (n - 3, 1), (n - 2, 2), (n - 2, 3)):
+        assert torch.equal(k[:, at], fill[p][0]) and torch.equal(v[:, at], fill[p][1])
