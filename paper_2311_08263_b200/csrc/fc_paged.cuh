@@ -399,19 +399,24 @@ cudaError_t by_lines(const PagedAttnArgs &all, int keys, F launch) {
   return cudaSuccess;
 }
 
-// The line, a piece for every warp, and the kernel that joins its parts; or clusters where the plan says so.
+// The line, a piece for every warp, and the kernel that joins its parts.
 template <int HD, int Q, int KEYS, typename K>
-cudaError_t launch_units(PagedAttnArgs a, const PagedPlan &plan, K line, K cluster, size_t smem, bool (*done)[kMaxDevices], cudaStream_t st) {
+cudaError_t launch_line(PagedAttnArgs a, const PagedPlan &plan, K line, size_t smem, bool *done, cudaStream_t st) {
   if (plan.queries != Q || plan.keys != KEYS) return cudaErrorInvalidValue;
   set_groups(a, Q);
-  if (plan.ctas == 0) {
-    if (cudaError_t e = allow_smem(line, smem, done[0])) return e;
-    return by_lines(a, KEYS, [&](const PagedAttnArgs &part) {
-      line<<<kSms, kPagedWarps * 32, smem, st>>>(part);
-      if (cudaError_t e = cudaGetLastError()) return e;
-      return launch_combine<HD, Q, KEYS>(part, plan.workers, st);
-    });
-  }
+  if (cudaError_t e = allow_smem(line, smem, done)) return e;
+  return by_lines(a, KEYS, [&](const PagedAttnArgs &part) {
+    line<<<kSms, plan.workers / kSms * 32, smem, st>>>(part);
+    if (cudaError_t e = cudaGetLastError()) return e;
+    return launch_combine<HD, Q, KEYS>(part, plan.workers, st);
+  });
+}
+// The same, or clusters where the plan says so.
+template <int HD, int Q, int KEYS, typename K>
+cudaError_t launch_units(PagedAttnArgs a, const PagedPlan &plan, K line, K cluster, size_t smem, bool (*done)[kMaxDevices], cudaStream_t st) {
+  if (plan.ctas == 0) return launch_line<HD, Q, KEYS>(a, plan, line, smem, done[0], st);
+  if (plan.queries != Q || plan.keys != KEYS) return cudaErrorInvalidValue;
+  set_groups(a, Q);
   if (cudaError_t e = allow_smem(cluster, smem, done[1])) return e;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);

@@ -112,7 +112,7 @@ struct PagedPlan {
   size_t scratch;         // bytes; 0 with clusters
   bool fits;              // one sequence's tiles can be counted
 };
-constexpr int kPagedSms = 148, kPagedWarps = 8, kUmmaQueries = 128, kUmmaKeys = 64, kMmaKeys = 16;
+constexpr int kPagedSms = 148, kPagedWarps = 8, kMoreWarps = 12, kUmmaQueries = 128, kUmmaKeys = 64, kMmaKeys = 16;
 constexpr size_t kUmmaStatus = (kPagedSms * sizeof(unsigned int) + 255) / 256 * 256;
 
 // CTAs of a cluster per unit where one launch of clusters does the work of the line and the kernel that joins its parts, 0 otherwise.  All
@@ -138,6 +138,11 @@ inline bool umma_pays(int batch, int n_kv_heads, int nq, int hd, long long most_
   return umma < mma;
 }
 
+// Warps per SM on the line of k_paged_attn.cu: more of them hide each other's waits where there is much to do; where there is little they leave more parts.  Measured,
+// 8 and 12 warps, by tiles per warp of 8: 7 (1 sequence x 4 kv heads over 32000 keys, hd 64) 14.5, 16.5 us; 5.5 (4 x 32 x 16 queries over 800, hd 128) 22.5, 24.1; 13.5 (8 x 8 over
+// 4000) 30.2, 29.7; 18 (8 x 40 x 16 over 1024) 50.9, 48.4; 35 (8 x 40 x 4 over 2052) 61.8, 59.8.  (10 warps 53.8 and 60.7; 16, at hd 64, as 12 or slower.)
+inline bool more_warps_pay(long long units, long long most_keys) { return units * (most_keys / kMmaKeys) >= 10ll * kPagedSms * kPagedWarps; }
+
 inline PagedPlan paged_plan(int batch, int c, int hq, int hkv, int hd, bool f32, int cap, int window, int n_sink) {
   PagedPlan p;
   const int nq = hq / hkv * c;
@@ -147,7 +152,7 @@ inline PagedPlan paged_plan(int batch, int c, int hq, int hkv, int hd, bool f32,
   p.keys = p.kind == kUmma ? kUmmaKeys : p.kind == kFma ? 1024 / hd : kMmaKeys;
   p.units = hkv * ((nq + p.queries - 1) / p.queries);
   p.ctas = p.kind == kUmma ? 0 : paged_cluster(batch, p.units, most, p.keys);
-  p.workers = p.kind == kUmma ? kPagedSms : kPagedSms * kPagedWarps;
+  p.workers = kPagedSms * (p.kind == kUmma ? 1 : p.kind == kMma && more_warps_pay((long long)batch * p.units, most) ? kMoreWarps : kPagedWarps);
   p.scratch = p.ctas ? 0 : (p.kind == kUmma ? kUmmaStatus : 0) + (size_t)p.workers * 2 * part_floats(p.queries, hd) * sizeof(float);
   p.fits = line_batch(p.units, cap, p.keys) > 0;
   return p;

@@ -5,7 +5,7 @@
 // head elements, always full, and only its 8 columns are queries.  A warp loads its own tiles into its own ring (cp.async, 16 bytes a lane; the
 // lanes look up the pages of the tile's keys, a tile ahead), so that it waits for nobody while it streams.  Scores, probabilities and the output
 // stay in its registers.
-//   Line: one CTA per SM, eight warps.  The tiles of all units stand in one line, sequence by sequence, cut into equal pieces, one per warp,
+//   Line: one CTA per SM, eight or twelve warps (more_warps_pay).  The tiles of all units stand in one line, sequence by sequence, cut into equal pieces, one per warp,
 // whatever the lengths: the launch depends on none, a batch of ragged caches is as balanced as one long cache, and the rings run on from unit to
 // unit.  A unit that several warps share goes to scratch as un-normalised sums, which paged_combine_kernel adds up in order.
 //   (A piece per CTA, whose warps take turns at its tiles and exchange sums where a unit ends, leaves fewer parts but stalls at every end: 7B, 16 x 1 token over
@@ -23,16 +23,19 @@ namespace fc {
 namespace {
 
 constexpr int kKeys = kMmaKeys;        // per tile
-constexpr int kWarps = kPagedWarps, kThreads = kWarps * 32;
 
-template <int HD>
+// W: warps of a CTA
+template <int HD, int W>
 struct PagedCfg {
+  static constexpr int kThreads = W * 32;
   static constexpr int kRow = HD * 2;                              // bytes of a key
   static constexpr uint32_t kHalf = kKeys * kRow, kTile = 2 * kHalf;
-  static constexpr int S = HD == 128 ? 3 : 6;                      // stages of a warp's ring
+  static constexpr int S = HD == 32 ? 6 : HD == 64 ? 48 / W : 24 / W;      // stages of a warp's ring: 192 KB, 96 at hd 32
   static constexpr int DB = HD / 16;                               // blocks of 16 elements of the output
-  static constexpr uint32_t kRing = kWarps * S * kTile;
-  static constexpr uint32_t kExchange = DB * (kWarps - 1) * 512;   // a block of 8 queries at a time
+  static constexpr uint32_t kRing = W * S * kTile;
+  // Of a cluster, a block of 8 queries at a time.  The line of eight warps asks for it too: SMs are then set to all the shared memory they can have, and the joining
+  // kernel's blocks fit in beside (1 sequence x 4 kv heads over 32000 keys 14.5 us, 15.6 without); twelve warps are faster alone (8 x 40 x 16 queries over 1024 48.4, 50.6).
+  static constexpr uint32_t kExchange = W > kPagedWarps ? 0 : DB * (W - 1) * 512;
   static constexpr size_t kSmem = 128 + kRing + kExchange;
 };
 
@@ -43,11 +46,11 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   return r;
 }
 
-// QN: blocks of 8 queries of a unit.  LINE: the line of tiles, else a cluster per unit (grid: CTAs of the cluster, units, sequences).
-template <int HD, int QN, bool LINE>
-__global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_constant__ PagedAttnArgs a) {
-  using C = PagedCfg<HD>;
-  constexpr int W = kWarps, S = C::S, KS = HD / 16, DB = C::DB, Q = 8 * QN;
+// QN: blocks of 8 queries of a unit.  W: warps.  LINE: the line of tiles, else a cluster per unit (grid: CTAs of the cluster, units, sequences).
+template <int HD, int QN, int W, bool LINE>
+__global__ void __launch_bounds__(W * 32, 1) paged_mma_kernel(const __grid_constant__ PagedAttnArgs a) {
+  using C = PagedCfg<HD, W>;
+  constexpr int S = C::S, KS = HD / 16, DB = C::DB, Q = 8 * QN;
   constexpr int PER = HD / 8;                            // 16-byte pieces of a row
   constexpr int OWN = (DB + W - 1) / W;                  // blocks of elements that a warp adds up
   if (LINE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -351,14 +354,17 @@ __global__ void __launch_bounds__(kThreads, 1) paged_mma_kernel(const __grid_con
   }
   if (gridDim.x == 1) return;
   const int q0 = seg.qg * Q;
-  join_cluster<HD>(a, seg, q0, min(Q, nq - q0), base, smem_u32(ml_cta), kThreads);
+  join_cluster<HD>(a, seg, q0, min(Q, nq - q0), base, smem_u32(ml_cta), C::kThreads);
 }
 
 // ------------------------------------------------------------------------------------ host side
 template <int HD, int QN>
 cudaError_t launch_mma(const PagedAttnArgs &a, const PagedPlan &plan, cudaStream_t st) {
-  static bool done[2][kMaxDevices] = {};
-  return launch_units<HD, 8 * QN, kKeys>(a, plan, paged_mma_kernel<HD, QN, true>, paged_mma_kernel<HD, QN, false>, PagedCfg<HD>::kSmem, done, st);
+  constexpr int W = kPagedWarps, M = kMoreWarps;
+  static bool done[2][kMaxDevices] = {}, more_done[kMaxDevices] = {};
+  if (plan.ctas == 0 && plan.workers == kSms * M)
+    return launch_line<HD, 8 * QN, kKeys>(a, plan, paged_mma_kernel<HD, QN, M, true>, PagedCfg<HD, M>::kSmem, more_done, st);
+  return launch_units<HD, 8 * QN, kKeys>(a, plan, paged_mma_kernel<HD, QN, W, true>, paged_mma_kernel<HD, QN, W, false>, PagedCfg<HD, W>::kSmem, done, st);
 }
 template <int HD>
 cudaError_t launch_hd(const PagedAttnArgs &a, const PagedPlan &plan, cudaStream_t st) {

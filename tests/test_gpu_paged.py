@@ -815,3 +815,51 @@ def test_copies_beyond_32_bits():
     assert table.tolist() == [[3, -1], [2, -1], [0, 1]] and refs[:4].tolist() == [1] * 4 and refs[4:].sum() == 0
     for p, at in ((0, 0), (n - 3, 1), (n - 2, 2), (n - 2, 3)):
         assert torch.equal(k[:, at], fill[p][0]) and torch.equal(v[:, at], fill[p][1])
+
+
+MORE = [
+    # hq, hkv, hd, c, page, layout, lens, window, sinks: up to 32 queries per kv head over tables that may hold much
+    (4, 4, 32, 8, 16, "hnd", EDGES, 0, 0),
+    (8, 2, 32, 7, 5, "padded", EDGES, 0, 0),
+    (8, 2, 64, 1, 16, "nhd", EDGES, 0, 0),
+    (8, 2, 64, 5, 24, "turns", EDGES, 0, 0),
+    (8, 8, 128, 1, 32, "turns", EDGES, 0, 0),
+    (8, 8, 128, 16, 16, "hnd", EDGES, 0, 0),
+    (6, 2, 128, 9, 1000, "nhd", [999, 998, 1000, 0, -1], 0, 0),
+    (8, 2, 64, 4, 16, "nhd", EDGES, 20, 4),
+    (8, 8, 128, 2, 7, "hnd", [500, 90, 3], 64, 1),
+    (4, 4, 32, 3, 16, "hnd", EDGES, 1, 0),
+]
+
+
+@pytest.mark.parametrize("case", range(len(MORE)))
+def test_lines_of_more_warps(case):
+    hq, hkv, hd, c, ps, order, lens, window, n_sink = MORE[case]
+    k, v, table, kv_len = _cache(lens, c, hkv, hd, ps, torch.bfloat16, order, 300 + case, window, n_sink)
+    rep = -(-8000 // (len(lens) * hkv)) if window else 1                     # under a window: the same sequences again
+    table = table if window else _widened(table, ps, 1 << 17)
+    queries = 8 if hq // hkv * c <= 8 else 16
+    want = 256 + 148 * 12 * 2 * queries * (hd + 2) * 4                       # the scratch of twelve warps per SM
+    assert lib.load().fc_op_paged_attention_scratch_bytes(len(lens) * rep, c, hq, hkv, hd, lib.FC_BF16, table.shape[1], ps, window, n_sink) == want
+    q = _queries(len(lens) * c, hq * hd, torch.bfloat16, case)
+    res = ref.attention(q, k, v, table, kv_len, c, hq, window, n_sink)
+    out = engine.fc_op_paged_attention(q.repeat(rep, 1), k, v, table.repeat(rep, 1), kv_len.repeat(rep), c, hq, window=window, n_sink=n_sink)
+    _close(out, *(x.repeat(rep, 1, 1) for x in res))
+
+
+@pytest.mark.parametrize("hd,ps,c", [(64, 16, 8), (128, 24, 16), (32, 5, 3)])
+def test_lines_of_more_warps_and_long_pieces(hd, ps, c):
+    """Rings used many times, units that end inside pieces; and a value that is not finite in the window's last row."""
+    hq, hkv, lens = 4, 4, [1500, 1400, 655, 3, 0, 900, 1111, 64] * 10
+    gen = torch.Generator().manual_seed(hd)
+    table, n_pages = _dealt(lens, c, ps, gen)
+    k, v = (torch.randn(n_pages, hkv, ps, hd, generator=gen).to(torch.bfloat16).cuda() for _ in range(2))
+    table, kv_len = table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+    q = _queries(len(lens) * c, hq * hd, torch.bfloat16, 1)
+    good = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq)
+    _close(good, *ref.attention(q, k, v, table, kv_len, c, hq))
+    tab = table.tolist()
+    for b, n in enumerate(lens):
+        v[tab[b][(n + c - 1) // ps], :, (n + c - 1) % ps, ::3] = math.nan
+    out = engine.fc_op_paged_attention(q, k, v, table, kv_len, c, hq).view(len(lens), c, -1, hd)
+    assert torch.equal(out[:, :-1], good.view(out.shape)[:, :-1]) and out[:, -1, :, ::3].isnan().all() and out[:, -1, :, 1::3].isfinite().all()

@@ -355,3 +355,11 @@ def test_plans(parts):
                        ((1, 16, 32, 8, 128, 0, 4016, 0, 0), 1), ((8, 32, 40, 40, 128, 0, 1056, 0, 0), 1), ((1, 16, 32, 4, 64, 0, 657, 0, 0), 1),
                        ((4, 51, 32, 32, 128, 0, 64, 0, 0), 1)):
         assert _plan(parts, *args)["kind"] == kind
+
+
+def test_workers_of_a_line(parts):
+    """Twelve warps per SM where the table may hold ten tiles and more for each of eight, on bf16 only; one CTA per SM with tcgen05."""
+    for args, workers in (((1, 1, 32, 4, 64, 0, 32064, 0, 0), 8), ((8, 16, 40, 40, 128, 0, 1056, 0, 0), 12), ((4, 16, 32, 32, 128, 0, 832, 0, 0), 8),
+                          ((8, 4, 40, 40, 128, 0, 16032, 2048, 4), 12), ((16, 1, 32, 32, 128, 1, 2064, 0, 0), 8), ((16, 16, 32, 4, 64, 0, 4112, 0, 0), 1)):
+        p = _plan(parts, *args)
+        assert p["ctas"] == 0 and p["workers"] == 148 * workers
