@@ -126,10 +126,10 @@ inline int paged_cluster(int batch, int units, long long most_keys, int keys) {
 
 // Whether tcgen05 pays: its units are 128 queries, used or not, and it starts and ends slowly.  By what both cost (microseconds, keys up to the
 // table's bound): 5 and 0.168 (hd 64) or 0.232 (hd 128) per 16 queries x 16 keys and SM, against 12 and 1.09 or 2.3 per unit's tile of 64 keys and SM.
-// Measured, mma.sync against tcgen05, sequences x kv heads x queries: hd 128, 4 x 32 x 64 over 1000 keys 59.6, 44.0; 8 x 8 x 64 over 2000 57.1, 41.7; 8 x 40 x 64 over
-// 1024 132.8, 96.0; 1 x 8 x 128 over 4000 35.0, 31.6; 1 x 8 x 64 over 4000 25.2, 28.4; 1 x 8 x 128 over 1000 13.5, 19.8; hd 64, 16 x 4 x 128 over 4000 125.3, 36.7,
-// over 641 29.2, 20.9; 8 x 4 x 64 over 2000 23.8, 21.0; 4 x 4 x 128 over 641 15.4, 16.5; 1 x 4 x 128 over 641 7.8, 12.7.  (Chosen wrongly by up to 9 %: hd 128, 2 x 8 x 64
-// over 2000 23.8, 22.0; 4 x 8 x 128 over 500 27.8, 30.3.)
+// Measured, mma.sync against tcgen05, sequences x kv heads x queries: hd 128, 4 x 32 x 64 over 1000 keys 61.7, 43.7; 8 x 8 x 64 over 2000 58.5, 41.9; 8 x 40 x 64 over
+// 1024 135, 95.5; 1 x 8 x 128 over 4000 37.0, 31.8; 1 x 8 x 64 over 4000 25.0, 28.4; 1 x 8 x 128 over 1000 13.3, 19.7; hd 64, 16 x 4 x 128 over 4000 105, 36.8,
+// over 641 27.7, 20.8; 8 x 4 x 64 over 2000 23.6, 21.1; 4 x 4 x 128 over 641 15.1, 16.4; 1 x 4 x 128 over 641 7.7, 12.7.  (Chosen wrongly by up to 10 %: hd 128, 2 x 8 x 64
+// over 2000 23.6, 22.0; 4 x 8 x 128 over 500 27.5, 30.3.)
 inline bool umma_pays(int batch, int n_kv_heads, int nq, int hd, long long most_keys) {
   if (nq <= 32 || hd < 64) return false;
   const double heads = (double)batch * n_kv_heads / kPagedSms;
