@@ -253,7 +253,7 @@ __device__ __forceinline__ void join_cluster(const PagedAttnArgs &a, const Place
 
 // ------------------------------------------------------------------------------------ joining the parts of a unit
 // A block takes block_rows queries of a unit: with items = queries x hd / 4 pieces of four elements, threads are groups that take turns at the
-// parts.  A few units have many parts each (one sequence, four kv heads: 37), and then a query per block reads them all at once.
+// parts.  A few units have many parts each (one sequence, four kv heads, 32000 keys: some 290), and then a query per block reads them all at once.
 
 constexpr int kCombine = 256;
 // U: parts that a thread has on their way at once.
