@@ -90,6 +90,12 @@ FC_ANY UnitParts unit_parts(int begin, int n, int chunk) {
 }
 FC_ANY int part_place(int begin, int worker, int chunk) { return begin > worker * chunk; }
 
+// Where a line's tiles are loaded by copies, kCopyWarps warps take turns at them (k_paged_umma.cu).  The queries of a segment go into one of two places,
+// behind the products of the segment but one in front of it, for which the loading warp waits with a parity: that tells a phase only from the ones next to it,
+// so the warp must have waited for all phases before.  Hence one warp loads the queries of all segments, whoever copies their first tile.
+constexpr int kCopyWarps = 2;
+FC_ANY int query_copier(int first_tile) { return 0; }
+
 // x / n for 0 <= x < 2^16, n < 2^16, by the reciprocal of n.
 FC_ANY unsigned int reciprocal16(int n) { return n == 1 ? 0u : (unsigned int)((0x100000000ull + (unsigned int)n - 1) / (unsigned int)n); }
 FC_ANY int quotient16(int x, unsigned int inv) { return inv ? (int)((unsigned long long)(unsigned int)x * inv >> 32) : x; }

@@ -24,7 +24,6 @@ namespace {
 
 constexpr int kKeys = kUmmaKeys, kQueries = kUmmaQueries;
 constexpr int kThreads = 384;
-constexpr int kCopyWarps = 2;                            // that load tiles where TMA does not
 
 template <int HD>
 struct UmmaCfg {
@@ -377,14 +376,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         landed();
         return mbar_wait_warp(bar, parity, quit);
       };
-      if (lw < n_mine) so += move_on<kKeys>(a, ld, lw);
-      for (int i = lw; i < n_mine; i += kCopyWarps) {
+      // the next tile; where it begins a segment, one of the warps loads that one's queries (query_copier says why it is always the same)
+      auto step = [&](int tile) {
+        if (!move_on<kKeys>(a, ld, 1)) return;
+        ++so;
+        if (lw != query_copier(tile)) return;
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        landed();                                        // the products that the wait is for may need them
+        ok = load_queries(ld, so);
+      };
+      if (lw == query_copier(0)) ok = load_queries(ld, 0);
+      for (int t = 1; t <= lw && t < n_mine; ++t) step(t);
+      for (int i = lw; ok && i < n_mine; i += kCopyWarps) {
         const int st = i % S;
-        if (ld.t == 0 || i == 0) {
-          asm volatile("cp.async.wait_group 0;" ::: "memory");
-          landed();
-          if (!load_queries(ld, so)) { ok = false; break; }
-        }
         // ---- pages of the lanes' keys (lane, lane + 32)
         const int see_from = window_first(ld.len + quotient16(ld.qg * kQueries, a.group_inv), a.window);
         const int see_to = min(ld.len + quotient16(min(nq - 1, ld.qg * kQueries + kQueries - 1), a.group_inv), a.cap - 1);
@@ -425,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         landed();
         pending = st;
-        if (i + kCopyWarps < n_mine) so += move_on<kKeys>(a, ld, kCopyWarps);
+        for (int t = i + 1; ok && t <= i + kCopyWarps && t < n_mine; ++t) step(t);
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
       if (ok) landed();
