@@ -35,6 +35,9 @@ struct PagedAttnArgs {
   unsigned int *status;   // scratch of the kernel that has waits, else null: per worker, 1 where a wait ran out
 };
 
+// Elements of a page are counted in 32 bits.
+FC_ANY bool page_too_large(int n_kv_heads, int page_size, int hd) { return (long long)n_kv_heads * page_size > (1ll << 31) / hd; }
+
 // Length of a sequence as the kernels use it: -1 for none, never far beyond the table's `cap` positions (no sum overflows).
 FC_ANY int clamp_len(int len, int cap) { return len < 0 ? -1 : len > cap ? cap : len; }
 

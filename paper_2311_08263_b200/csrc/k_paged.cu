@@ -79,12 +79,17 @@ __global__ void __launch_bounds__(256) paged_store_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------------------ arguments
+// FC_OK, or why a call's numbers are refused, whatever its pool looks like otherwise.
+int shape_ok(int width, int page_size, int hkv, int hd, int batch, int c, int hq) {
+  if (width < 1 || page_size < 1 || hkv < 1 || batch < 1 || c < 1 || c > 64 || hq < 1 || hq % hkv) return FC_ERR_ARG;
+  if (hd != 32 && hd != 64 && hd != 128) return FC_ERR_SHAPE;
+  if (page_too_large(hkv, page_size, hd) || (long long)width * page_size > INT_MAX - 1024 || (long long)batch * c * hq > INT_MAX / 2 || hq > 512) return FC_ERR_CAPACITY;
+  return FC_OK;
+}
 int call_ok(const fc_pages *pages, int layer, const int32_t *table, int width, const int32_t *kv_len, int batch, int c, int hq) {
   if (int rc = pages_ok(pages)) return rc;
-  if (!table || !kv_len || layer < 0 || layer >= pages->n_layers || width < 1 || batch < 1 || c < 1 || c > 64 || hq < 1) return FC_ERR_ARG;
-  if (hq % pages->n_kv_heads) return FC_ERR_ARG;
-  if ((long long)width * pages->page_size > INT_MAX - 1024 || (long long)batch * c * hq > INT_MAX / 2 || hq > 512) return FC_ERR_CAPACITY;
-  return FC_OK;
+  if (!table || !kv_len || layer < 0 || layer >= pages->n_layers) return FC_ERR_ARG;
+  return shape_ok(width, pages->page_size, pages->n_kv_heads, pages->head_dim, batch, c, hq);
 }
 
 PageView view_of(const fc_pages *p, int layer) {
@@ -136,9 +141,7 @@ constexpr size_t kNoScratch = 256;
 
 extern "C" size_t fc_op_paged_attention_scratch_bytes(int32_t batch, int32_t c, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                                       int32_t dtype, int32_t table_width, int32_t page_size, int32_t window, int32_t n_sink) {
-  if (batch < 1 || c < 1 || c > 64 || n_heads < 1 || n_heads > 512 || n_kv_heads < 1 || n_heads % n_kv_heads) return 0;
-  if ((head_dim != 32 && head_dim != 64 && head_dim != 128) || (dtype != FC_F32 && dtype != FC_BF16)) return 0;
-  if (table_width < 1 || page_size < 1 || (long long)table_width * page_size > INT_MAX - 1024 || window < 0 || n_sink < 0) return 0;
+  if (shape_ok(table_width, page_size, n_kv_heads, head_dim, batch, c, n_heads) || (dtype != FC_F32 && dtype != FC_BF16) || window < 0 || n_sink < 0) return 0;
   const PagedPlan plan = paged_plan(batch, c, n_heads, n_kv_heads, head_dim, dtype == FC_F32, table_width * page_size, window, window > 0 ? n_sink : 0);
   return !plan.fits ? 0 : plan.scratch == 0 ? kNoScratch : kNoScratch + (plan.scratch + 255) / 256 * 256;
 }

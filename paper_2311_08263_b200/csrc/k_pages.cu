@@ -359,7 +359,7 @@ int pages_ok(const fc_pages *p) {
   if (p->dtype != FC_F32 && p->dtype != FC_BF16) return FC_ERR_ARG;
   if (p->n_layers < 1 || p->n_pages < 1 || p->n_kv_heads < 1 || p->page_size < 1) return FC_ERR_ARG;
   if (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) return FC_ERR_SHAPE;
-  if ((long long)p->n_kv_heads * p->page_size > (1ll << 31) / p->head_dim) return FC_ERR_CAPACITY;       // elements of a page: 32 bits
+  if (page_too_large(p->n_kv_heads, p->page_size, p->head_dim)) return FC_ERR_CAPACITY;
   const int per = p->dtype == FC_F32 ? 4 : 8;
   if (((uintptr_t)p->k | (uintptr_t)p->v) % 16) return FC_ERR_ARG;
   long long count[4] = {p->n_layers, p->n_pages, p->n_kv_heads, p->page_size};
