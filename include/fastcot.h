@@ -315,8 +315,9 @@ int fc_op_paged_store(const fc_pages *pages, int32_t layer, const int32_t *table
  * and values are in their slots already.  q: [batch * c] rows of n_heads * head_dim in the pool's type, q_stride elements apart; out: fp32
  * [batch * c, n_heads * head_dim].  Rows of a table row without a sequence are 0.  A row that sees a key whose page is not in the
  * pool, or lies beyond the table, is NaN; pages that no row sees may be missing.  Keys and values that a row does not see do not reach
- * it, whatever they hold.  Scores of minus infinity weigh nothing; a row that has no other is NaN.  Results do not depend on the order in which
- * the work runs.
+ * it, whatever they hold.  A row that sees a value that is not finite has no finite result in that element; whether an infinite value leaves
+ * infinity or NaN there is not said.  Scores of minus infinity weigh nothing; a row that has no other is NaN.  Results do not depend on the
+ * order in which the work runs.
  * (The waits inside its kernels are bounded; should one run out, which no argument or content causes, the rows that it concerns are NaN.)
  * c <= 64, n_heads <= 512 (else, and for tables of some ten million positions and many heads, FC_ERR_CAPACITY); q, out 16-byte aligned, q_stride a
  * multiple of 16 bytes; scratch: device, 256-byte aligned, at least ..._scratch_bytes(...) bytes for these arguments, whatever the lengths; what it holds

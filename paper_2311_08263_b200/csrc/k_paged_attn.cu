@@ -16,6 +16,8 @@
 //
 // Probabilities enter the tensor cores as three bf16 parts (their sum has all 24 bits), a tile's product is added to the output in fp32: what is rounded
 // is what is stored in the cache, nothing else.  (Two parts leave 1.5e-6, relative, of the result.)
+// An infinite value that a row sees becomes NaN where it meets parts of zero or of the other sign, which only tiles that some row does not see whole
+// rule out (their values that are not finite are added by FMA): no finite result either way, and more is not promised.
 #include "fc_paged.cuh"
 
 namespace fc {
