@@ -334,7 +334,15 @@ def _rows(x: torch.Tensor):
     return (row, elem) if x.shape[0] > 1 else (x.shape[1], elem)
 
 
+def _in_int32(*numbers: int) -> None:
+    """ctypes drops the bits beyond 32 without a word; what C refuses within them (negative numbers among it) is left to C."""
+    if max(numbers) > 0x7fffffff or min(numbers) < -0x80000000:
+        raise ValueError("numbers beyond 32 bits")
+
+
 def _list(ids):
+    if len(ids):
+        _in_int32(*ids)
     return (C.c_int32 * len(ids))(*ids)
 
 
@@ -376,6 +384,7 @@ def fc_op_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tab
                           n_heads: int, window: int = 0, n_sink: int = 0) -> torch.Tensor:
     """Window attention of one layer over pages, optionally under a sliding window with sinks.  q [B*c, n_heads * hd] in the pool's type,
     rows adjacent or not; the rest as in fc_op_paged_store, the rows' own keys and values stored.  Returns fp32 [B*c, n_heads * hd]."""
+    _in_int32(window, n_sink)
     pool, device = _pool(k, v, 4), k.get_device()
     tab = _ints("table", table, 2, device)
     B, width = table.shape
@@ -393,6 +402,7 @@ def fc_op_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tab
 
 def fc_op_pages_fork(table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, page_size: int, src, dst) -> None:
     """Table rows dst[i] share the pages of rows src[i]'s committed tokens (lists of row numbers on the host)."""
+    _in_int32(page_size, refs.numel())
     device, (rows, width), n = table.get_device(), table.shape, len(dst)
     if len(src) != n:
         raise ValueError("src and dst: two lists of the same length")
@@ -403,6 +413,7 @@ def fc_op_pages_fork(table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tens
 def fc_op_pages_free(table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, page_size: int, seqs, window: int = 0,
                      n_sink: int = 0) -> None:
     """Release the pages of table rows `seqs` (a list on the host): all of them, or those that no later row of a sliding window sees."""
+    _in_int32(page_size, refs.numel(), window, n_sink)
     device, (rows, width) = table.get_device(), table.shape
     _enqueue(device, _l.load().fc_op_pages_free, _ints("table", table, 2, device), width, rows, _lengths(kv_len, rows, device),
              _ints("refs", refs, 1, device), refs.numel(), page_size, _list(seqs), len(seqs), window, n_sink)
@@ -412,6 +423,7 @@ def fc_op_pages_reserve(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k
                         rows: int) -> torch.Tensor:
     """Pages for positions kv_len .. kv_len + rows - 1 of every sequence, copies of shared ones.  k/v [layers, pages, n_kv_heads, slots, hd].
     Returns int32 [n_seqs]: 1 where the positions can be written."""
+    _in_int32(rows, rows)
     pool, device = _pool(k, v, 5), k.get_device()
     tab, counts = _ints("table", table, 2, device), _ints("refs", refs, 1, device)
     n, width = table.shape
