@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
       // ------------------------------------------------------------------------------------------ tiles by cp.async, two warps in turn
       const int lw = warp - 9;
       Place ld = seg;
-      int pending = -1, so = 0;
+      int pending = -1, so = -1;
       bool ok = true;
       auto landed = [&]() {                              // the copies of `pending` are here: for the tensor core to read
         if (pending < 0) return;
@@ -376,18 +376,17 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         landed();
         return mbar_wait_warp(bar, parity, quit);
       };
-      // the next tile; where it begins a segment, one of the warps loads that one's queries (query_copier says why it is always the same)
-      auto step = [&](int tile) {
-        if (!move_on<kKeys>(a, ld, 1)) return;
-        ++so;
-        if (lw != query_copier(tile)) return;
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        landed();                                        // the products that the wait is for may need them
-        ok = load_queries(ld, so);
-      };
-      if (lw == query_copier(0)) ok = load_queries(ld, 0);
-      for (int t = 1; t <= lw && t < n_mine; ++t) step(t);
-      for (int i = lw; ok && i < n_mine; i += kCopyWarps) {
+      bool begins = true;                                // tile i is the first of a segment
+      for (int i = 0, on; i < n_mine; i += on, begins = i < n_mine && move_on<kKeys>(a, ld, on) > 0) {
+        so += begins;
+        if (begins && lw == query_copier(i)) {           // always the same warp, whose tile it is or not
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          landed();                                      // the products that the wait is for may need them
+          if (!load_queries(ld, so)) { ok = false; break; }
+        }
+        on = 1;
+        if (i % kCopyWarps != lw) continue;
+        if (ld.t + kCopyWarps < ld.k.n) on = kCopyWarps; // nothing begins at the other warp's tile
         const int st = i % S;
         // ---- pages of the lanes' keys (lane, lane + 32)
         const int see_from = window_first(ld.len + quotient16(ld.qg * kQueries, a.group_inv), a.window);
@@ -429,7 +428,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_umma_kernel(const __grid_co
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         landed();
         pending = st;
-        for (int t = i + 1; ok && t <= i + kCopyWarps && t < n_mine; ++t) step(t);
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
       if (ok) landed();
