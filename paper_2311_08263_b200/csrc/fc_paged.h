@@ -138,7 +138,9 @@ inline int paged_cluster(int batch, int units, long long most_keys, int keys) {
 // Measured, mma.sync against tcgen05, sequences x kv heads x queries: hd 128, 4 x 32 x 64 over 1000 keys 61.7, 43.7; 8 x 8 x 64 over 2000 58.5, 41.9; 8 x 40 x 64 over
 // 1024 135, 95.5; 1 x 8 x 128 over 4000 37.0, 31.8; 1 x 8 x 64 over 4000 25.0, 28.4; 1 x 8 x 128 over 1000 13.3, 19.7; hd 64, 16 x 4 x 128 over 4000 105, 36.8,
 // over 641 27.7, 20.8; 8 x 4 x 64 over 2000 23.6, 21.1; 4 x 4 x 128 over 641 15.1, 16.4; 1 x 4 x 128 over 641 7.7, 12.7.  (Chosen wrongly by up to 10 %: hd 128, 2 x 8 x 64
-// over 2000 23.6, 22.0; 4 x 8 x 128 over 500 27.5, 30.3.)
+// over 2000 23.6, 22.0; 4 x 8 x 128 over 500 27.5, 30.3.)  All of that in tables as wide as their caches: only the table's width is known here, and a table for much
+// more than its sequences hold gets the form for long ones (hd 64, 1 x 4 x 128 over 641 keys in a table for 4096
+// positions: 12.7 us on tcgen05, 7.5 in clusters in one for 2048).
 inline bool umma_pays(int batch, int n_kv_heads, int nq, int hd, long long most_keys) {
   if (nq <= 32 || hd < 64) return false;
   const double heads = (double)batch * n_kv_heads / kPagedSms;

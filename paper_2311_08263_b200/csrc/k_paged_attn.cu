@@ -32,7 +32,7 @@ struct PagedCfg {
   static constexpr int kThreads = W * 32;
   static constexpr int kRow = HD * 2;                              // bytes of a key
   static constexpr uint32_t kHalf = kKeys * kRow, kTile = 2 * kHalf;
-  static constexpr int S = HD == 32 ? 6 : HD == 64 ? 48 / W : 24 / W;      // stages of a warp's ring: 192 KB, 96 at hd 32
+  static constexpr int S = HD == 32 ? 6 : HD == 64 ? 48 / W : 24 / W;      // stages of a warp's ring: 192 KB in all, at hd 32 96 or (12 warps) 144
   static constexpr int DB = HD / 16;                               // blocks of 16 elements of the output
   static constexpr uint32_t kRing = W * S * kTile;
   // Of a cluster, a block of 8 queries at a time.  The line of eight warps asks for it too: SMs are then set to all the shared memory they can have, and the joining

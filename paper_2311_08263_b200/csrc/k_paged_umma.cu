@@ -12,6 +12,8 @@
 //     keys where the heads of a group divide 128: the keys' warp runs tiles ahead, and a box of them is here sooner than 128 rows of copies).
 // Measured (hd 64, 16 sequences x 4 kv heads x 128 queries, 3640 keys on average): 34.9 us with the join, 0.22 PFLOP/s, or 0.44 with the parts; K/V at 1.75 TB/s.  Bound by the
 // latency of the softmax: two warps per scheduler issue in 40 % of the cycles, the tensor pipe is 20 % busy.
+// Spills, in bytes stored and loaded: 324 and 300 at hd 64, 564 and 600 at hd 128 by TMA; 308 and 272, 516 and 544 by copies.  (Compiled without the code for tiles
+// that some row does not see whole 184 and 188, 440 and 508 by TMA; without the third group none: 168 registers are what all threads start with.)
 // Every wait is bounded: where one runs out the CTA says so in its status word, and the joining kernel writes NaN for what it was to compute.
 #include <type_traits>
 
